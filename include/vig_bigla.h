@@ -9,9 +9,9 @@
  *     The one exception is the measurement aid at the end of this header: vig_timing_enable(1)
  *     creates a pool of HIP events, and vig_timing_collect waits for them.
  *   - Tensors are dense, row-major, innermost index = feature.  All tensors of one call
- *     share `dtype` (vig_dtype).  VIG_BF16: bf16 in, fp32 accumulate, bf16 out rounded to
+ *     share `dtype` (vig_dtype), but for the states and statistics that are FP32 where said.  VIG_BF16: bf16 in, fp32 accumulate, bf16 out rounded to
  *     nearest even.  VIG_F32: fp32 throughout.
- *   - Every tensor pointer must be 16-byte aligned; outputs must not alias inputs.
+ *   - Every tensor pointer must be 16-byte aligned; outputs must not alias inputs (unless said).
  *   - Return value: a vig_status.  Arguments are validated on the host before anything is
  *     launched; nothing aborts or throws across this boundary.  After VIG_ERR_HIP the raw
  *     hipError_t is available from vig_last_hip_error().
@@ -30,8 +30,10 @@ typedef enum {
     VIG_ERR_NULL = -1,        /* a required pointer is NULL                              */
     VIG_ERR_SHAPE = -2,       /* a size is <= 0 or the product of sizes overflows        */
     VIG_ERR_DTYPE = -3,       /* dtype is not a vig_dtype                                */
-    VIG_ERR_UNSUPPORTED = -4, /* dk or dv outside {16, 32, 64}; D not a multiple of 32;
-                                 a plan the shape does not admit                         */
+    VIG_ERR_UNSUPPORTED = -4, /* dk or dv outside {16, 32, 64} (gated delta rule: or 128); D not a
+                                 multiple of 32; heads or channels not a multiple of their
+                                 groups; a plan the shape does not admit; a direction or an
+                                 activation that is none                                 */
     VIG_ERR_ALIGN = -5,       /* a pointer is not 16-byte aligned                        */
     VIG_ERR_WORKSPACE = -6,   /* workspace NULL or smaller than bigla_workspace_bytes()  */
     VIG_ERR_HIP = -7,         /* a HIP call failed; see vig_last_hip_error()             */
@@ -312,6 +314,84 @@ int gated_bigla_fwd(const void *x, const void *w1, const void *w2, const void *b
                     void *stream);
 
 /*
+ * Gated delta rule -- a token mixer like bigla_fwd's, one scan direction a call, whose write first takes off what the state
+ * answers for the key already.  For every batch element b and head h, with alpha_t = exp(g_t) (one gate per token):
+ *     e_t = v_t - alpha_t k_t S_{t-1} ,   S_t = alpha_t S_{t-1} + beta_t k_t^T e_t ,   out_t = q_t S_t
+ * that is S_t = alpha_t (I - beta_t k_t^T k_t) S_{t-1} + beta_t k_t^T v_t.  With VIG_SCAN_BACKWARD the scan starts at the last
+ * token (t + 1 stands for t - 1); a bidirectional mixer is two calls.  No scaling or normalisation of q and k is applied.
+ *
+ *   q, k           [B, Hk, L, dk]    in    Hk divides H: the heads h of H / Hk consecutive ones share key head h / (H / Hk)
+ *   v              [B, H, L, dv]     in
+ *   g, beta        [B, H, L]         in    LOG forget gates (<= 0; -infinity resets the state) and write strengths
+ *   initial_state  [B, H, dk, dv]    in    FP32 for either dtype; NULL: zero
+ *   out            [B, H, L, dv]     out
+ *   final_state    [B, H, dk, dv]    out   FP32 for either dtype; NULL: not wanted; may be initial_state
+ *   (or [B, L, H, d] and [B, L, H] with VIG_LAYOUT_BLHD; states are the same in both); dk, dv in {16, 32, 64, 128}; any L >= 1;
+ *   H below 2^17.  Values are finite (gates excepted), as is beta_t |k_t|^2 in [0, 2] where a bounded state is wanted.  A token
+ *   with g = 0 and beta = 0 leaves the state as it is: so are padded ones marked.
+ *   workspace: at least gated_delta_workspace_bytes(...) bytes (the chunks' matrices), which is 0 for invalid sizes.
+ * Chunks of 64 tokens, on the matrix cores for both dtypes.  VIG_BF16: every intermediate operand in two bf16 parts (16 bits), in
+ * three (24 bits) where a final state is asked for; VIG_F32: fp32 operands.
+ */
+typedef enum { VIG_SCAN_FORWARD = 0, VIG_SCAN_BACKWARD = 1 } vig_scan;
+size_t gated_delta_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, int dtype);
+int gated_delta_fwd(const void *q, const void *k, const void *v, const void *g, const void *beta, const void *initial_state,
+                    void *out, void *final_state, int B, int H, int Hk, int L, int dk, int dv, int dtype, int layout,
+                    int direction, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The gradient of gated_delta_fwd.  With D_t the gradient of S_t (q_t^T d_out_t added, later tokens' in it; D after the last token is
+ * d_final_state):
+ *     r_t = k_t D_t ,  dv_t = beta_t r_t ,  dbeta_t = r_t . e_t ,  dq_t = d_out_t S_t^T ,
+ *     dk_t = beta_t e_t D_t^T - beta_t alpha_t r_t S_{t-1}^T ,  D'_t = D_t - beta_t k_t^T r_t ,
+ *     dg_t = <D'_t, alpha_t S_{t-1}> ,  alpha_t D'_t enters D_{t-1}
+ *   q, k, v, g, beta, initial_state          as for gated_delta_fwd                          in
+ *   d_out [B, H, L, dv]; d_final_state [B, H, dk, dv] FP32 or NULL (zero)                    in
+ *   dq, dk [B, Hk, L, dk] (summed over the heads that share a key head), dv [B, H, L, dv], dg, dbeta [B, H, L]      out
+ *   d_initial_state [B, H, dk, dv] FP32 or NULL (not wanted)                                 out
+ *   workspace: at least gated_delta_bwd_workspace_bytes(...) bytes (the chunks' matrices, two states per chunk, two fp32
+ *   rows of dv values per token).  Results do not depend on how the work is spread: no atomics.
+ */
+size_t gated_delta_bwd_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, int dtype);
+int gated_delta_bwd(const void *q, const void *k, const void *v, const void *g, const void *beta, const void *initial_state,
+                    const void *d_out, const void *d_final_state, void *dq, void *dk, void *dv, void *dg, void *dbeta,
+                    void *d_initial_state, int B, int H, int Hk, int L, int dk_, int dv_, int dtype, int layout, int direction,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The gated delta rule for one token of each of B sequences, their states updated in place in a pool.
+ *   q, k [B, Hk, dk], v [B, H, dv], g, beta [B, H]   in
+ *   state [n_slots, H, dk, dv] FP32                  in and out
+ *   slots [B] int32 or NULL                          in    sequence b has the state slots[b]; NULL: state b (n_slots >= B).  A slot
+ *                                                          outside [0, n_slots) marks a padded row: its output is zero and no
+ *                                                          state is touched.  Slots of one call are distinct.
+ *   out [B, H, dv]                                   out
+ */
+int gated_delta_step(const void *q, const void *k, const void *v, const void *g, const void *beta, void *state,
+                     const int *slots, void *out, int B, int H, int Hk, int dk, int dv, int n_slots, int dtype, void *stream);
+
+/*
+ * Channels-last group norm with an activation: what is applied to a token-major output (a group per head) or to the grids of
+ * the convolutions around a mixer.  Group j of element b holds the channels [j C / groups, (j + 1) C / groups) of all L positions:
+ *     xn = (x - mean) / sqrt(var + eps) ,   out = act(xn * weight + bias)         (var: mean squared distance from the mean)
+ *   x, out        [B, L, C]         C a multiple of 8 and of groups, up to VIG_GROUP_NORM_MAX_CHANNELS
+ *   weight, bias  [C], or both NULL (one and zero)
+ *   stats         [B, groups, 2]    out   FP32 for either dtype: mean and 1 / sqrt(var + eps), what the gradient takes
+ *   eps > 0; act a vig_act (VIG_ACT_SILU: z / (1 + exp(-z))); fp32 arithmetic for either dtype.
+ *   workspace: at least group_norm_workspace_bytes(...) bytes (0 where a group fits one workgroup's registers, and for invalid sizes).
+ * group_norm_act_bwd: from d_out = dLoss/dout, dx like x, d_weight and d_bias like weight (NULL exactly where weight is NULL).
+ */
+#define VIG_GROUP_NORM_MAX_CHANNELS 8192
+typedef enum { VIG_ACT_NONE = 0, VIG_ACT_SILU = 1 } vig_act;
+size_t group_norm_workspace_bytes(int B, int L, int C, int groups, int dtype);
+int group_norm_act_fwd(const void *x, const void *weight, const void *bias, void *out, void *stats, int B, int L, int C,
+                       int groups, float eps, int act, int dtype, void *workspace, size_t workspace_bytes, void *stream);
+size_t group_norm_bwd_workspace_bytes(int B, int L, int C, int groups, int dtype);
+int group_norm_act_bwd(const void *x, const void *weight, const void *bias, const void *stats, const void *d_out, void *dx,
+                       void *d_weight, void *d_bias, int B, int L, int C, int groups, int act, int dtype, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/*
  * Measurement aid (no part of the method): per-kernel timing with HIP events recorded on the
  * stream each kernel is launched on.  vig_timing_enable(1) clears the records and makes every
  * later launch of this library from the calling thread record a start/stop event pair;
@@ -328,7 +408,12 @@ typedef enum {
     VIG_KERNEL_SEGMENT_OUT_GENERAL = 5, /* chunkwise path, output pass of single-chunk sequences */
     VIG_KERNEL_GATE_PRODUCER = 6, /* forget-gate producer                                     */
     VIG_KERNEL_SLAB = 7,          /* chunkwise path, one-segment plans: both passes, one launch */
-    VIG_KERNEL_BACKWARD = 8       /* all launches of one bigla_bwd call together               */
+    VIG_KERNEL_BACKWARD = 8,      /* all launches of one bigla_bwd call together               */
+    VIG_KERNEL_GATED_DELTA = 9,   /* all launches of one gated_delta_fwd call together         */
+    VIG_KERNEL_GATED_DELTA_BACKWARD = 10, /* ... of one gated_delta_bwd call                   */
+    VIG_KERNEL_GATED_DELTA_STEP = 11,
+    VIG_KERNEL_GROUP_NORM = 12,   /* all launches of one group_norm_act_fwd call together      */
+    VIG_KERNEL_GROUP_NORM_BACKWARD = 13 /* ... of one group_norm_act_bwd call                  */
 } vig_kernel;
 int vig_timing_enable(int on);
 int vig_timing_collect(int kernel, double *total_ms, long *launches);

@@ -26,16 +26,23 @@ LAYOUTS = {"bhld": VIG_LAYOUT_BHLD, "blhd": VIG_LAYOUT_BLHD}
 PLANS = {"auto": 0, "two_launches": 1, "fused_epilogue": 2}
 FWD_PLANS = {"auto": 0, "four_wave": 1, "wave_specialised": 2, "slab_sweep": 3}
 GATES_PLANS = {"auto": 0, "separate": 1, "in_state_pass": 2}
+SCANS = {"forward": 0, "backward": 1}
+ACTS = {"none": 0, "silu": 1}
 
 # every symbol include/vig_bigla.h declares
 EXPORTS = ("bigla_workspace_bytes", "bigla_fwd", "bigla_fwd_layout", "bigla_fwd_plan", "bigla_fwd_static_scratch", "locality_gate_fwd",
            "locality_gate_fwd_layout", "bigla_locality_workspace_bytes", "bigla_locality_fwd", "gate_producer_fwd",
            "gated_bigla_workspace_bytes", "gated_bigla_fwd",
            "bigla_bwd_workspace_bytes", "bigla_bwd", "bigla_bwd_plan",
+           "gated_delta_workspace_bytes", "gated_delta_fwd", "gated_delta_bwd_workspace_bytes", "gated_delta_bwd",
+           "gated_delta_step", "group_norm_workspace_bytes", "group_norm_act_fwd", "group_norm_bwd_workspace_bytes",
+           "group_norm_act_bwd",
            "vig_status_str", "vig_last_hip_error", "vig_timing_enable",
            "vig_timing_collect", "vig_measure_alias_slabs")
 KERNELS = {"segment_state": 0, "gate_lowrank": 1, "segment_out": 2, "recurrent": 3, "locality_gate": 4,
-           "segment_out_general": 5, "gate_producer": 6, "slab": 7, "backward": 8}
+           "segment_out_general": 5, "gate_producer": 6, "slab": 7, "backward": 8,
+           "gated_delta": 9, "gated_delta_backward": 10, "gated_delta_step": 11, "group_norm": 12,
+           "group_norm_backward": 13}
 
 _lib = None
 
@@ -85,6 +92,24 @@ def lib() -> ctypes.CDLL:
         L.gated_bigla_workspace_bytes.restype = sz
         L.gated_bigla_fwd.argtypes = [vp] * 10 + [ci] * 6 + [ctypes.c_float, ci, ci, ci, vp, sz, vp]
         L.gated_bigla_fwd.restype = ci
+        L.gated_delta_workspace_bytes.argtypes = [ci] * 7
+        L.gated_delta_workspace_bytes.restype = sz
+        L.gated_delta_fwd.argtypes = [vp] * 8 + [ci] * 9 + [vp, sz, vp]
+        L.gated_delta_fwd.restype = ci
+        L.gated_delta_bwd_workspace_bytes.argtypes = [ci] * 7
+        L.gated_delta_bwd_workspace_bytes.restype = sz
+        L.gated_delta_bwd.argtypes = [vp] * 14 + [ci] * 9 + [vp, sz, vp]
+        L.gated_delta_bwd.restype = ci
+        L.gated_delta_step.argtypes = [vp] * 8 + [ci] * 7 + [vp]
+        L.gated_delta_step.restype = ci
+        L.group_norm_workspace_bytes.argtypes = [ci] * 5
+        L.group_norm_workspace_bytes.restype = sz
+        L.group_norm_act_fwd.argtypes = [vp] * 5 + [ci] * 4 + [ctypes.c_float, ci, ci, vp, sz, vp]
+        L.group_norm_act_fwd.restype = ci
+        L.group_norm_bwd_workspace_bytes.argtypes = [ci] * 5
+        L.group_norm_bwd_workspace_bytes.restype = sz
+        L.group_norm_act_bwd.argtypes = [vp] * 8 + [ci] * 6 + [vp, sz, vp]
+        L.group_norm_act_bwd.restype = ci
         L.vig_status_str.argtypes = [ci]
         L.vig_status_str.restype = ctypes.c_char_p
         L.vig_last_hip_error.argtypes = []
@@ -433,6 +458,185 @@ def gated_bigla_fwd(x, w1, w2, q, k, v, bias=None, tau: float = 16.0, layout="bh
                                    workspace.numel() * workspace.element_size(), _stream_ptr(q.device))
     _check(st, "gated_bigla_fwd")
     return out, g_fwd, g_bwd
+
+
+def _fp32(t, name, shape, like):
+    """An fp32 tensor (a state, statistics) beside tensors of either dtype."""
+    t = _dev(t, name, shape)
+    if t.dtype != torch.float32 or t.device != like.device:
+        raise VigError(VIG_ERR_DTYPE, f"{name} must be float32, on the device of the other tensors")
+    return t
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _workspace(workspace, need: int, device):
+    """(workspace, bytes): the caller's, or one allocated with torch where some is needed."""
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace is not None:
+        workspace = _dev(workspace, "workspace")
+        if workspace.device != device:
+            raise VigError(VIG_ERR_DTYPE, "workspace must be on the device of the other tensors")
+    return workspace, workspace.numel() * workspace.element_size() if workspace is not None else 0
+
+
+def _delta_args(q, k, v, g, beta, layout, direction):
+    lay = _layout_code(layout)
+    if direction not in SCANS:
+        raise VigError(VIG_ERR_UNSUPPORTED, f"direction must be one of {sorted(SCANS)}")
+    q, v = _dev(q, "q"), _dev(v, "v")
+    if q.dim() != 4 or v.dim() != 4:
+        raise VigError(VIG_ERR_SHAPE, "q and v must be 4-dimensional")
+    if lay == VIG_LAYOUT_BHLD:
+        (B, Hk, L, dk), H = q.shape, v.shape[1]
+    else:
+        (B, L, Hk, dk), H = q.shape, v.shape[2]
+    dv = v.shape[3]
+    heads = (B, H, L) if lay == VIG_LAYOUT_BHLD else (B, L, H)
+    _dev(k, "k", q.shape, q)
+    _dev(v, "v", heads + (dv,), q)
+    _dev(g, "g", heads, q)
+    _dev(beta, "beta", heads, q)
+    return (B, H, Hk, L, dk, dv, _dtype_code(q)), lay, SCANS[direction]
+
+
+def gated_delta_workspace_bytes(B: int, H: int, Hk: int, L: int, dk: int, dv: int, dtype: int) -> int:
+    return int(lib().gated_delta_workspace_bytes(B, H, Hk, L, dk, dv, dtype))
+
+
+def gated_delta_fwd(q, k, v, g, beta, initial_state=None, return_final_state=False, out=None, final_state=None,
+                    workspace=None, layout="bhld", direction="forward"):
+    """Gated delta rule: S_t = exp(g_t) (I - beta_t k_t^T k_t) S_{t-1} + beta_t k_t^T v_t, out_t = q_t S_t.
+
+    q, k: [B,Hk,L,dk] with Hk dividing H; v: [B,H,L,dv]; g (log gates), beta: [B,H,L] (layout "bhld"), or [B,L,H,...]
+    (layout "blhd"); initial_state: float32 [B,H,dk,dv] or None (zero).  direction "backward" scans from the last token.
+    Returns out, or (out, final_state) where the final state is asked for (return_final_state, or a tensor for it, which
+    may be initial_state).
+    """
+    sizes, lay, scan = _delta_args(q, k, v, g, beta, layout, direction)
+    B, H, Hk, L, dk, dv, code = sizes
+    if initial_state is not None:
+        _fp32(initial_state, "initial_state", (B, H, dk, dv), q)
+    if final_state is None and return_final_state:
+        final_state = torch.empty((B, H, dk, dv), dtype=torch.float32, device=q.device)
+    if final_state is not None:
+        _fp32(final_state, "final_state", (B, H, dk, dv), q)
+    out = torch.empty_like(v) if out is None else _dev(out, "out", v.shape, q)
+    workspace, ws_bytes = _workspace(workspace, gated_delta_workspace_bytes(*sizes), q.device)
+    with _on_device(q.device):
+        st = lib().gated_delta_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(),
+                                   _ptr(initial_state), out.data_ptr(), _ptr(final_state), *sizes, lay, scan,
+                                   _ptr(workspace), ws_bytes, _stream_ptr(q.device))
+    _check(st, "gated_delta_fwd")
+    return out if final_state is None else (out, final_state)
+
+
+def gated_delta_bwd(q, k, v, g, beta, d_out, initial_state=None, d_final_state=None, workspace=None, layout="bhld",
+                    direction="forward"):
+    """Gradient of gated_delta_fwd: (dq, dk, dv, dg, dbeta) for the output gradient d_out (shaped like v) and, where given,
+    the gradient d_final_state of the final state; with an initial_state its gradient follows as a sixth tensor (float32)."""
+    sizes, lay, scan = _delta_args(q, k, v, g, beta, layout, direction)
+    B, H, Hk, L, dk, dv, code = sizes
+    _dev(d_out, "d_out", v.shape, q)
+    d_initial = None
+    if initial_state is not None:
+        _fp32(initial_state, "initial_state", (B, H, dk, dv), q)
+        d_initial = torch.empty_like(initial_state)
+    if d_final_state is not None:
+        _fp32(d_final_state, "d_final_state", (B, H, dk, dv), q)
+    grads = tuple(torch.empty_like(t) for t in (q, k, v, g, beta))
+    workspace, ws_bytes = _workspace(workspace, int(lib().gated_delta_bwd_workspace_bytes(*sizes)), q.device)
+    with _on_device(q.device):
+        st = lib().gated_delta_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(),
+                                   _ptr(initial_state), d_out.data_ptr(), _ptr(d_final_state),
+                                   *(t.data_ptr() for t in grads), _ptr(d_initial), *sizes, lay, scan, _ptr(workspace),
+                                   ws_bytes, _stream_ptr(q.device))
+    _check(st, "gated_delta_bwd")
+    return grads if d_initial is None else grads + (d_initial,)
+
+
+def gated_delta_step(q, k, v, g, beta, state, slots=None, out=None):
+    """The gated delta rule for one token of each of B sequences; `state` (float32 [n_slots,H,dk,dv]) is updated in place.
+
+    q, k: [B,Hk,dk]; v: [B,H,dv]; g, beta: [B,H]; slots: int32 [B], the state of each sequence (distinct; one outside
+    [0, n_slots) marks a padded row, whose output is zero), or None (sequence b has state b) -> out [B,H,dv].
+    """
+    q, v, state = _dev(q, "q"), _dev(v, "v"), _dev(state, "state")
+    if q.dim() != 3 or v.dim() != 3 or state.dim() != 4:
+        raise VigError(VIG_ERR_SHAPE, "q and v must be 3-dimensional, state 4-dimensional")
+    (B, Hk, dk), (_, H, dv) = q.shape, v.shape
+    _dev(k, "k", q.shape, q)
+    _dev(v, "v", (B, H, dv), q)
+    _dev(g, "g", (B, H), q)
+    _dev(beta, "beta", (B, H), q)
+    n_slots = state.shape[0]
+    _fp32(state, "state", (n_slots, H, dk, dv), q)
+    if slots is not None:
+        _dev(slots, "slots", (B,))
+        if slots.dtype != torch.int32 or slots.device != q.device:
+            raise VigError(VIG_ERR_DTYPE, "slots must be int32, on the device of the other tensors")
+    out = torch.empty_like(v) if out is None else _dev(out, "out", v.shape, q)
+    with _on_device(q.device):
+        st = lib().gated_delta_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(),
+                                    state.data_ptr(), _ptr(slots), out.data_ptr(), B, H, Hk, dk, dv, n_slots,
+                                    _dtype_code(q), _stream_ptr(q.device))
+    _check(st, "gated_delta_step")
+    return out
+
+
+def _norm_args(x, groups, weight, bias, act):
+    if act not in ACTS:
+        raise VigError(VIG_ERR_UNSUPPORTED, f"act must be one of {sorted(ACTS)}")
+    x = _dev(x, "x")
+    if x.dim() < 2:
+        raise VigError(VIG_ERR_SHAPE, "x must be [B, ..., C]")
+    B, C = x.shape[0], x.shape[-1]
+    if B == 0 or C == 0 or x.numel() == 0:
+        raise VigError(VIG_ERR_SHAPE, "x has no elements")
+    if (weight is None) != (bias is None):
+        raise VigError(VIG_ERR_NULL, "weight and bias come together")
+    if weight is not None:
+        _dev(weight, "weight", (C,), x)
+        _dev(bias, "bias", (C,), x)
+    return (B, x.numel() // (B * C), C, groups), _dtype_code(x), ACTS[act]
+
+
+def group_norm_act_fwd(x, groups: int, weight=None, bias=None, eps: float = 1e-5, act="silu", out=None, stats=None,
+                       workspace=None):
+    """Channels-last group norm and activation: act((x - mean) / sqrt(var + eps) * weight + bias), the statistics over all
+    positions and the C / groups channels of a group.  x: [B, ..., C]; weight, bias: [C] or both None; act: "silu" or "none".
+    Returns (out, stats), stats: float32 [B, groups, 2], mean and 1 / sqrt(var + eps), for group_norm_act_bwd."""
+    sizes, code, act_code = _norm_args(x, groups, weight, bias, act)
+    out = torch.empty_like(x) if out is None else _dev(out, "out", x.shape, x)
+    if stats is None:
+        stats = torch.empty((sizes[0], max(groups, 0), 2), dtype=torch.float32, device=x.device)
+    _fp32(stats, "stats", (sizes[0], groups, 2), x)
+    workspace, ws_bytes = _workspace(workspace, int(lib().group_norm_workspace_bytes(*sizes, code)), x.device)
+    with _on_device(x.device):
+        st = lib().group_norm_act_fwd(x.data_ptr(), _ptr(weight), _ptr(bias), out.data_ptr(), stats.data_ptr(), *sizes,
+                                      float(eps), act_code, code, _ptr(workspace), ws_bytes, _stream_ptr(x.device))
+    _check(st, "group_norm_act_fwd")
+    return out, stats
+
+
+def group_norm_act_bwd(x, d_out, stats, groups: int, weight=None, bias=None, act="silu", workspace=None):
+    """Gradient of group_norm_act_fwd: (dx, d_weight, d_bias) for the output gradient d_out and the forward's stats
+    (d_weight and d_bias are None without a weight)."""
+    sizes, code, act_code = _norm_args(x, groups, weight, bias, act)
+    _dev(d_out, "d_out", x.shape, x)
+    _fp32(stats, "stats", (sizes[0], groups, 2), x)
+    dx = torch.empty_like(x)
+    dw, db = (torch.empty_like(weight), torch.empty_like(bias)) if weight is not None else (None, None)
+    workspace, ws_bytes = _workspace(workspace, int(lib().group_norm_bwd_workspace_bytes(*sizes, code)), x.device)
+    with _on_device(x.device):
+        st = lib().group_norm_act_bwd(x.data_ptr(), _ptr(weight), _ptr(bias), stats.data_ptr(), d_out.data_ptr(),
+                                      dx.data_ptr(), _ptr(dw), _ptr(db), *sizes, act_code, code, _ptr(workspace), ws_bytes,
+                                      _stream_ptr(x.device))
+    _check(st, "group_norm_act_bwd")
+    return dx, dw, db
 
 
 def timing_enable(on: bool) -> None:

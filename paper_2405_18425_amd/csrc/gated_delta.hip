@@ -1,0 +1,75 @@
+// Gated delta rule, forward: gd_prepare for the chunks' matrices, gd_states for the chain.
+#include "gated_delta_chain.hpp"
+#include "gated_delta_prepare.hpp"
+#include "vig_kernels.hpp"
+#include "vig_timing.hpp"
+
+namespace vig {
+
+namespace {
+
+using namespace gd;
+
+// Parts of a 32-bit operand: a returned state takes three, bf16 results two
+template <typename T, int DK>
+size_t fwd_bytes(const Shape &s, bool states)
+{
+    const size_t units = size_t(s.B) * s.H * s.chunks, key_units = size_t(s.B) * s.Hk * s.chunks;
+    const size_t chunk = states ? ChunkWs<T, 3, false>::bytes : ChunkWs<T, 2, false>::bytes;
+    return round256(units * chunk) + round256(key_units * KeyWs<T, DK, false>::bytes);
+}
+
+template <typename T, int DK, int N>
+hipError_t launch(const Shape &s, const void *q, const void *k, const void *v, const void *g, const void *beta, const float *initial, void *out,
+                  float *final_state, void *workspace, hipStream_t stream)
+{
+    const unsigned slabs = unsigned(s.B) * unsigned(s.H), units = slabs * unsigned(s.chunks);
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    unsigned char *key_ws = ws + round256(size_t(units) * ChunkWs<T, N, false>::bytes);
+    const PrepareArgs<T> p = {s, static_cast<const T *>(q), static_cast<const T *>(k), static_cast<const T *>(g), static_cast<const T *>(beta), ws, key_ws};
+    const ChainArgs<T> c = {s, p.q, p.k, static_cast<const T *>(v), initial, static_cast<T *>(out), final_state, nullptr, nullptr, ws, key_ws};
+    const LaunchTimer timer(kKernelGatedDelta, stream);
+    gd_prepare<T, DK, N, false><<<units, 256, 0, stream>>>(p);
+    gd_states<T, DK, N><<<(slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 64, 0, stream>>>(c);
+    return hipGetLastError();
+}
+
+template <typename T, int DK, typename... A>
+hipError_t launch_parts(bool states, const Shape &s, A... rest)
+{
+    if constexpr (sizeof(T) == 2)
+        if (states) return launch<T, DK, 3>(s, rest...);
+    return launch<T, DK, 2>(s, rest...);
+}
+
+template <typename T, typename... A>
+hipError_t launch_width(bool states, const Shape &s, A... rest)
+{
+    if (s.dk <= 32) return launch_parts<T, 32>(states, s, rest...);
+    if (s.dk <= 64) return launch_parts<T, 64>(states, s, rest...);
+    return launch_parts<T, 128>(states, s, rest...);
+}
+
+}  // namespace
+
+size_t gated_delta_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, bool is_bf16)
+{
+    const Shape s = {B, H, Hk, L, dk, dv, (L + kC - 1) / kC, false, false};
+    const auto of = [&](auto t) {
+        using T = decltype(t);
+        return dk <= 32 ? fwd_bytes<T, 32>(s, true) : dk <= 64 ? fwd_bytes<T, 64>(s, true) : fwd_bytes<T, 128>(s, true);
+    };
+    return is_bf16 ? of(bf16_t{}) : of(float{});
+}
+
+hipError_t gated_delta_launch(const void *q, const void *k, const void *v, const void *g, const void *beta, const float *initial, void *out,
+                              float *final_state, int B, int H, int Hk, int L, int dk, int dv, bool is_bf16, bool token_major, bool reverse,
+                              void *workspace, hipStream_t stream)
+{
+    const Shape s = {B, H, Hk, L, dk, dv, (L + kC - 1) / kC, token_major, reverse};
+    const bool states = final_state != nullptr;
+    if (is_bf16) return launch_width<bf16_t>(states, s, q, k, v, g, beta, initial, out, final_state, workspace, stream);
+    return launch_width<float>(states, s, q, k, v, g, beta, initial, out, final_state, workspace, stream);
+}
+
+}  // namespace vig

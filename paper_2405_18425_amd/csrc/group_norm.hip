@@ -1,0 +1,557 @@
+// Channels-last group norm with an activation, and its gradient.  x is [B, L, C]; group j of element b holds the channels jC/G .. and all L
+// positions, N = L C / G values:
+//     xn = (x - mean) rstd,  z = xn w + b,  y = act(z),   mean, rstd = (var + eps)^-1/2 per (b, j)
+//     da = dy act'(z),  dw = sum da xn,  db = sum da  (over b and L),   dx = rstd (da w - m1 - xn m2),
+//     m1 = mean of da w, m2 = mean of da w xn over the group.
+//
+// Bound by memory: x in, y out (x, dy in, dx out).  A group of few values is held in the registers of one workgroup: one launch, x is
+// read once.  Otherwise two launches: partial sums of strips of rows over all channels, then the result, whose workgroups join the strips' sums of their
+// element themselves (the same order in each, so results do not depend on the launch); the second reading of x comes from
+// the Infinity Cache up to its size.  A thread owns 16 bytes of channels of every RG-th row, so a wave reads whole rows whatever the group width.
+//
+// Variances are sums of squared distances, never a difference of large sums: a thread's values are taken relative to the first of
+// them, threads and strips are joined by their means.
+#include "vig_common.hpp"
+#include "vig_kernels.hpp"
+#include "vig_timing.hpp"
+
+namespace vig {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+template <typename T>
+constexpr int kVec = 16 / int(sizeof(T));
+
+template <typename T>
+struct Values {
+    float v[kVec<T>];
+};
+__device__ __forceinline__ void load(Values<bf16_t> &x, const bf16_t *p)
+{
+    const u32x4 u = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.v[2 * j] = bf16_lo_to_f32(u[j]), x.v[2 * j + 1] = bf16_hi_to_f32(u[j]);
+}
+__device__ __forceinline__ void load(Values<float> &x, const float *p)
+{
+    const f32x4 u = *reinterpret_cast<const f32x4 *>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.v[j] = u[j];
+}
+__device__ __forceinline__ void store(bf16_t *p, const Values<bf16_t> &x)
+{
+    u32x4 u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = pack2(x.v[2 * j], x.v[2 * j + 1]);
+    *reinterpret_cast<u32x4 *>(p) = u;
+}
+__device__ __forceinline__ void store(float *p, const Values<float> &x) { *reinterpret_cast<f32x4 *>(p) = f32x4{x.v[0], x.v[1], x.v[2], x.v[3]}; }
+
+// 1 / (1 + exp(-z)): the exponential overflows to infinity where the result is 0
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + fast_exp2(-1.4426950408889634f * z)); }
+template <bool kSilu>
+__device__ __forceinline__ float act(float z)
+{
+    return kSilu ? z * sigmoid(z) : z;
+}
+template <bool kSilu>
+__device__ __forceinline__ float act_slope(float z)
+{
+    if (!kSilu) return 1.f;
+    const float s = sigmoid(z);
+    return s * fmaf(z, 1.f - s, 1.f);
+}
+
+__device__ __forceinline__ float wave_sum(float x)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    return x;
+}
+
+struct Plan {
+    int B, L, C, G, strips, rows;  // rows of a strip
+    int vecs, row_groups;          // 16-byte pieces of a row; rows that a workgroup takes at a time
+};
+
+template <typename T>
+struct NormArgs {
+    Plan p;
+    const T *x, *weight, *bias;  // weight and bias may be null
+    T *out;
+    float *stats;                // [B, G, 2] mean, rstd
+    float eps;
+    float2 *partial;             // [B][strips][G] mean, sum of squared distances
+    // gradient
+    const float *in_stats;
+    const T *d_out;
+    T *d_weight, *d_bias;
+    float2 *channel;             // [B][strips][C] sums of da, da xn
+};
+
+template <typename T>
+__device__ __forceinline__ Values<T> vector_or(const T *p, int c, float value)
+{
+    Values<T> x;
+    if (p)
+        load(x, p + c);
+    else
+#pragma unroll
+        for (int j = 0; j < kVec<T>; ++j) x.v[j] = value;
+    return x;
+}
+
+// ---- a group per workgroup -------------------------------------------------------------------------
+
+template <typename T, int R /* pieces of a thread */, bool kSilu>
+__global__ __launch_bounds__(kThreads) void norm_group_kernel(NormArgs<T> a)
+{
+    constexpr int V = kVec<T>, kWaves = kThreads / 64;
+    __shared__ float part[2][kWaves];
+    const Plan &p = a.p;
+    const unsigned b = blockIdx.x / unsigned(p.G), j = blockIdx.x - b * unsigned(p.G);
+    const int width = p.C / p.G, pieces = width / V, all = p.L * pieces;
+    const size_t base = size_t(b) * p.L * p.C + size_t(j) * width;
+    const int w = threadIdx.x >> 6;
+    Values<T> x[R];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int at = int(threadIdx.x) + i * kThreads, row = at / pieces, c = (at - row * pieces) * V;
+        if (at < all)
+            load(x[i], a.x + base + size_t(row) * p.C + c);
+        else
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[i].v[e] = 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum += x[i].v[e];
+    }
+    const float n = float(p.L) * float(width);
+    sum = wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) part[0][w] = sum;
+    __syncthreads();
+    const float mean = ((part[0][0] + part[0][1]) + (part[0][2] + part[0][3])) / n;
+    float sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const bool there = int(threadIdx.x) + i * kThreads < all;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            x[i].v[e] -= mean;
+            sq = there ? fmaf(x[i].v[e], x[i].v[e], sq) : sq;
+        }
+    }
+    sq = wave_sum(sq);
+    if ((threadIdx.x & 63) == 0) part[1][w] = sq;
+    __syncthreads();
+    const float var = ((part[1][0] + part[1][1]) + (part[1][2] + part[1][3])) / n, rstd = 1.f / sqrtf(var + a.eps);
+    if (threadIdx.x == 0) *reinterpret_cast<float2 *>(a.stats + 2 * size_t(blockIdx.x)) = make_float2(mean, rstd);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int at = int(threadIdx.x) + i * kThreads, row = at / pieces, c = (at - row * pieces) * V;
+        if (at >= all) continue;
+        const Values<T> wt = vector_or(a.weight, int(j) * width + c, 1.f), bi = vector_or(a.bias, int(j) * width + c, 0.f);
+        Values<T> y;
+#pragma unroll
+        for (int e = 0; e < V; ++e) y.v[e] = act<kSilu>(fmaf(x[i].v[e], rstd * wt.v[e], bi.v[e]));
+        store(a.out + base + size_t(row) * p.C + c, y);
+    }
+}
+
+// ---- strips of rows --------------------------------------------------------------------------------
+
+__device__ __forceinline__ int rows_at(const Plan &p, int strip, int &first)
+{
+    first = strip * p.rows;
+    const int n = p.L - first;
+    return n < p.rows ? n : p.rows;
+}
+__device__ __forceinline__ int rows_of_group(int rows, int group, int groups) { return group < rows ? (rows - group + groups - 1) / groups : 0; }
+
+// Mean and squared distances of every group over the rows of a strip
+template <typename T>
+__global__ __launch_bounds__(kThreads) void norm_strip_kernel(NormArgs<T> a)
+{
+    constexpr int V = kVec<T>;
+    extern __shared__ __align__(16) float2 entry[];  // [row_groups][C] mean, squared distances
+    const Plan &p = a.p;
+    const unsigned b = blockIdx.x / unsigned(p.strips), strip = blockIdx.x - b * unsigned(p.strips);
+    int first;
+    const int rows = rows_at(p, int(strip), first);
+    const T *x = a.x + (size_t(b) * p.L + first) * p.C;
+    const int rg = p.row_groups > 1 ? int(threadIdx.x) / p.vecs : 0;
+    if (rg < p.row_groups)
+        for (int vec = p.row_groups > 1 ? int(threadIdx.x) - rg * p.vecs : int(threadIdx.x); vec < p.vecs; vec += kThreads) {
+            const int n = rows_of_group(rows, rg, p.row_groups);
+            float s1[V], s2[V];
+            Values<T> base, y;
+#pragma unroll
+            for (int e = 0; e < V; ++e) s1[e] = s2[e] = base.v[e] = 0.f;
+            const T *q = x + size_t(rg) * p.C + vec * V;
+            const size_t step = size_t(p.row_groups) * p.C;
+            if (n > 0) load(base, q);
+#pragma unroll 4
+            for (int i = 1; i < n; ++i) {
+                load(y, q + i * step);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float d = y.v[e] - base.v[e];
+                    s1[e] += d;
+                    s2[e] = fmaf(d, d, s2[e]);
+                }
+            }
+            const float inv = n > 0 ? 1.f / float(n) : 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                entry[rg * p.C + vec * V + e] = make_float2(fmaf(s1[e], inv, base.v[e]), fmaxf(fmaf(-s1[e] * inv, s1[e], s2[e]), 0.f));
+        }
+    __syncthreads();
+    const int lane = threadIdx.x & 63, width = p.C / p.G, entries = p.row_groups * width;
+    for (int j = threadIdx.x >> 6; j < p.G; j += kThreads / 64) {
+        float sum = 0.f;
+        for (int i = lane; i < entries; i += 64) {
+            const int g = i / width, c = i - g * width;
+            sum = fmaf(float(rows_of_group(rows, g, p.row_groups)), entry[g * p.C + j * width + c].x, sum);
+        }
+        const float mean = wave_sum(sum) / (float(rows) * float(width));
+        float sq = 0.f;
+        for (int i = lane; i < entries; i += 64) {
+            const int g = i / width, c = i - g * width;
+            const float2 v = entry[g * p.C + j * width + c];
+            const float d = v.x - mean;
+            sq += fmaf(float(rows_of_group(rows, g, p.row_groups)) * d, d, v.y);
+        }
+        sq = wave_sum(sq);
+        if (lane == 0) a.partial[size_t(blockIdx.x) * p.G + j] = make_float2(mean, sq);
+    }
+}
+
+template <typename T, bool kSilu>
+__global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs<T> a)
+{
+    constexpr int V = kVec<T>;
+    extern __shared__ __align__(16) float2 stat[];  // [G] mean, rstd
+    const Plan &p = a.p;
+    const unsigned b = blockIdx.x / unsigned(p.strips), strip = blockIdx.x - b * unsigned(p.strips);
+    const int lane = threadIdx.x & 63, width = p.C / p.G;
+    for (int j = threadIdx.x >> 6; j < p.G; j += kThreads / 64) {  // the strips' sums of the element
+        const float2 *part = a.partial + size_t(b) * p.strips * p.G + j;
+        int first;
+        float sum = 0.f;
+        for (int i = lane; i < p.strips; i += 64) sum = fmaf(float(rows_at(p, i, first)), part[size_t(i) * p.G].x, sum);
+        const float mean = wave_sum(sum) / float(p.L);
+        float sq = 0.f;
+        for (int i = lane; i < p.strips; i += 64) {
+            const float2 v = part[size_t(i) * p.G];
+            const float d = v.x - mean;
+            sq += fmaf(float(rows_at(p, i, first)) * float(width) * d, d, v.y);
+        }
+        const float rstd = 1.f / sqrtf(wave_sum(sq) / (float(p.L) * float(width)) + a.eps);
+        if (lane == 0) {
+            stat[j] = make_float2(mean, rstd);
+            if (strip == 0) *reinterpret_cast<float2 *>(a.stats + 2 * (size_t(b) * p.G + j)) = make_float2(mean, rstd);
+        }
+    }
+    __syncthreads();
+    int first;
+    const int rows = rows_at(p, int(strip), first);
+    const size_t at = (size_t(b) * p.L + first) * p.C;
+    const int rg = p.row_groups > 1 ? int(threadIdx.x) / p.vecs : 0;
+    if (rg >= p.row_groups) return;
+    for (int vec = p.row_groups > 1 ? int(threadIdx.x) - rg * p.vecs : int(threadIdx.x); vec < p.vecs; vec += kThreads) {
+        const int n = rows_of_group(rows, rg, p.row_groups);
+        Values<T> scale = vector_or(a.weight, vec * V, 1.f), bi = vector_or(a.bias, vec * V, 0.f);
+        float mean[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float2 v = stat[(vec * V + e) / width];
+            mean[e] = v.x;
+            scale.v[e] *= v.y;
+        }
+        const size_t from = at + size_t(rg) * p.C + vec * V, step = size_t(p.row_groups) * p.C;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            Values<T> y;
+            load(y, a.x + from + i * step);
+#pragma unroll
+            for (int e = 0; e < V; ++e) y.v[e] = act<kSilu>(fmaf(y.v[e] - mean[e], scale.v[e], bi.v[e]));
+            store(a.out + from + i * step, y);
+        }
+    }
+}
+
+// ---- gradient --------------------------------------------------------------------------------------
+
+template <typename T>
+struct Channels {  // what a thread needs of its channels
+    float mean[kVec<T>], rstd[kVec<T>], w[kVec<T>], b[kVec<T>];
+};
+template <typename T>
+__device__ __forceinline__ Channels<T> channels_at(const NormArgs<T> &a, unsigned b, int c)
+{
+    const Values<T> w = vector_or(a.weight, c, 1.f), bi = vector_or(a.bias, c, 0.f);
+    const int width = a.p.C / a.p.G;
+    Channels<T> ch;
+#pragma unroll
+    for (int e = 0; e < kVec<T>; ++e) {
+        const float2 v = *reinterpret_cast<const float2 *>(a.in_stats + 2 * (size_t(b) * a.p.G + (c + e) / width));
+        ch.mean[e] = v.x;
+        ch.rstd[e] = v.y;
+        ch.w[e] = w.v[e];
+        ch.b[e] = bi.v[e];
+    }
+    return ch;
+}
+
+// Sums of da and da xn over the rows of a strip: by channel, and weighted by group
+template <typename T, bool kSilu>
+__global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormArgs<T> a)
+{
+    constexpr int V = kVec<T>;
+    extern __shared__ __align__(16) float2 entry[];  // [row_groups][C]
+    const Plan &p = a.p;
+    const unsigned b = blockIdx.x / unsigned(p.strips), strip = blockIdx.x - b * unsigned(p.strips);
+    int first;
+    const int rows = rows_at(p, int(strip), first);
+    const size_t at = (size_t(b) * p.L + first) * p.C;
+    const int rg = p.row_groups > 1 ? int(threadIdx.x) / p.vecs : 0;
+    if (rg < p.row_groups)
+        for (int vec = p.row_groups > 1 ? int(threadIdx.x) - rg * p.vecs : int(threadIdx.x); vec < p.vecs; vec += kThreads) {
+            const int n = rows_of_group(rows, rg, p.row_groups);
+            const Channels<T> ch = channels_at(a, b, vec * V);
+            float s1[V], s2[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) s1[e] = s2[e] = 0.f;
+            const size_t from = at + size_t(rg) * p.C + vec * V, step = size_t(p.row_groups) * p.C;
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                Values<T> x, d;
+                load(x, a.x + from + i * step);
+                load(d, a.d_out + from + i * step);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float xn = (x.v[e] - ch.mean[e]) * ch.rstd[e], da = d.v[e] * act_slope<kSilu>(fmaf(xn, ch.w[e], ch.b[e]));
+                    s1[e] += da;
+                    s2[e] = fmaf(da, xn, s2[e]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) entry[rg * p.C + vec * V + e] = make_float2(s1[e], s2[e]);
+        }
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.C; c += kThreads) {
+        float2 s = entry[c];
+        for (int g = 1; g < p.row_groups; ++g) s.x += entry[g * p.C + c].x, s.y += entry[g * p.C + c].y;
+        a.channel[size_t(blockIdx.x) * p.C + c] = s;
+        const float w = a.weight ? io<T>::load(a.weight + c) : 1.f;
+        entry[c] = make_float2(s.x * w, s.y * w);  // (a thread's own channel: no other reads it before the barrier)
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 63, width = p.C / p.G;
+    for (int j = threadIdx.x >> 6; j < p.G; j += kThreads / 64) {
+        float s1 = 0.f, s2 = 0.f;
+        for (int c = lane; c < width; c += 64) s1 += entry[j * width + c].x, s2 += entry[j * width + c].y;
+        s1 = wave_sum(s1);
+        s2 = wave_sum(s2);
+        if (lane == 0) a.partial[size_t(blockIdx.x) * p.G + j] = make_float2(s1, s2);
+    }
+}
+
+// The first workgroups join the strips' channel sums (64 channels each), the others write dx
+template <typename T, bool kSilu>
+__global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormArgs<T> a, unsigned joins)
+{
+    constexpr int V = kVec<T>;
+    extern __shared__ __align__(16) float2 stat[];  // [G] m1, m2; or [4][64]
+    const Plan &p = a.p;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (blockIdx.x < joins) {
+        const int c = int(blockIdx.x) * 64 + lane;
+        float s1 = 0.f, s2 = 0.f;
+        if (c < p.C)
+#pragma unroll 8
+            for (int i = w; i < p.B * p.strips; i += kThreads / 64) {
+                const float2 v = a.channel[size_t(i) * p.C + c];
+                s1 += v.x;
+                s2 += v.y;
+            }
+        stat[w * 64 + lane] = make_float2(s1, s2);
+        __syncthreads();
+        if (w == 0 && c < p.C) {
+            const float2 u = stat[lane], v = stat[64 + lane], x = stat[128 + lane], y = stat[192 + lane];
+            io<T>::store(a.d_bias + c, (u.x + v.x) + (x.x + y.x));
+            io<T>::store(a.d_weight + c, (u.y + v.y) + (x.y + y.y));
+        }
+        return;
+    }
+    const unsigned block = blockIdx.x - joins, b = block / unsigned(p.strips), strip = block - b * unsigned(p.strips);
+    const int width = p.C / p.G;
+    for (int j = w; j < p.G; j += kThreads / 64) {
+        const float2 *part = a.partial + size_t(b) * p.strips * p.G + j;
+        float s1 = 0.f, s2 = 0.f;
+        for (int i = lane; i < p.strips; i += 64) s1 += part[size_t(i) * p.G].x, s2 += part[size_t(i) * p.G].y;
+        s1 = wave_sum(s1);
+        s2 = wave_sum(s2);
+        const float inv = 1.f / (float(p.L) * float(width));
+        if (lane == 0) stat[j] = make_float2(s1 * inv, s2 * inv);
+    }
+    __syncthreads();
+    int first;
+    const int rows = rows_at(p, int(strip), first);
+    const size_t at = (size_t(b) * p.L + first) * p.C;
+    const int rg = p.row_groups > 1 ? int(threadIdx.x) / p.vecs : 0;
+    if (rg >= p.row_groups) return;
+    for (int vec = p.row_groups > 1 ? int(threadIdx.x) - rg * p.vecs : int(threadIdx.x); vec < p.vecs; vec += kThreads) {
+        const int n = rows_of_group(rows, rg, p.row_groups);
+        const Channels<T> ch = channels_at(a, b, vec * V);
+        float2 m[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) m[e] = stat[(vec * V + e) / width];
+        const size_t from = at + size_t(rg) * p.C + vec * V, step = size_t(p.row_groups) * p.C;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            Values<T> x, d;
+            load(x, a.x + from + i * step);
+            load(d, a.d_out + from + i * step);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float xn = (x.v[e] - ch.mean[e]) * ch.rstd[e], da = d.v[e] * act_slope<kSilu>(fmaf(xn, ch.w[e], ch.b[e]));
+                d.v[e] = ch.rstd[e] * (fmaf(da, ch.w[e], -m[e].x) - xn * m[e].y);
+            }
+            store(a.out + from + i * step, d);
+        }
+    }
+}
+
+// ---- plans -----------------------------------------------------------------------------------------
+
+constexpr int kWorkgroups = 1024;  // four a compute unit
+
+Plan plan_of(int B, int L, int C, int G, int vec)
+{
+    Plan p = {B, L, C, G, 1, L, C / vec, 1};
+    if (p.vecs < kThreads) p.row_groups = kThreads / p.vecs;
+    // strips until the chip is full, of no fewer than four rows a thread
+    const int most = (L + 4 * p.row_groups - 1) / (4 * p.row_groups), want = (kWorkgroups + B - 1) / B;
+    p.strips = want < most ? want : most;
+    p.rows = (L + p.strips - 1) / p.strips;
+    p.strips = (L + p.rows - 1) / p.rows;
+    return p;
+}
+Plan plan_of(int B, int L, int C, int G, bool is_bf16) { return plan_of(B, L, C, G, is_bf16 ? 8 : 4); }
+
+constexpr int kMostPieces = 8;  // of a thread of norm_group_kernel
+
+bool group_in_registers(const Plan &p, int vec)
+{
+    const int width = p.C / p.G;
+    return width % vec == 0 && long(p.L) * (width / vec) <= long(kMostPieces) * kThreads;
+}
+
+template <typename T, bool kSilu>
+hipError_t forward(const NormArgs<T> &a, hipStream_t stream)
+{
+    const Plan &p = a.p;
+    const LaunchTimer timer(kKernelGroupNorm, stream);
+    if (group_in_registers(p, kVec<T>)) {
+        const int pieces = p.L * (p.C / p.G / kVec<T>), each = (pieces + kThreads - 1) / kThreads;
+        const unsigned grid = unsigned(p.B) * unsigned(p.G);
+        if (each <= 1)
+            norm_group_kernel<T, 1, kSilu><<<grid, kThreads, 0, stream>>>(a);
+        else if (each <= 2)
+            norm_group_kernel<T, 2, kSilu><<<grid, kThreads, 0, stream>>>(a);
+        else if (each <= 4)
+            norm_group_kernel<T, 4, kSilu><<<grid, kThreads, 0, stream>>>(a);
+        else
+            norm_group_kernel<T, 8, kSilu><<<grid, kThreads, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    const unsigned grid = unsigned(p.B) * unsigned(p.strips);
+    norm_strip_kernel<T><<<grid, kThreads, size_t(p.row_groups) * p.C * sizeof(float2), stream>>>(a);
+    norm_apply_kernel<T, kSilu><<<grid, kThreads, size_t(p.G) * sizeof(float2), stream>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, bool kSilu>
+hipError_t backward(const NormArgs<T> &a, hipStream_t stream)
+{
+    const Plan &p = a.p;
+    const LaunchTimer timer(kKernelGroupNormBackward, stream);
+    const unsigned grid = unsigned(p.B) * unsigned(p.strips), joins = a.d_weight ? unsigned(p.C + 63) / 64 : 0;
+    const size_t stat = size_t(p.G > 256 ? p.G : 256) * sizeof(float2);
+    norm_sums_kernel<T, kSilu><<<grid, kThreads, size_t(p.row_groups) * p.C * sizeof(float2), stream>>>(a);
+    norm_grad_kernel<T, kSilu><<<grid + joins, kThreads, stat, stream>>>(a, joins);
+    return hipGetLastError();
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+template <typename T>
+hipError_t forward_of(const void *x, const void *weight, const void *bias, void *out, float *stats, const Plan &p, float eps, bool silu, void *workspace,
+                      hipStream_t stream)
+{
+    NormArgs<T> a = {};
+    a.p = p;
+    a.x = static_cast<const T *>(x);
+    a.weight = static_cast<const T *>(weight);
+    a.bias = static_cast<const T *>(bias);
+    a.out = static_cast<T *>(out);
+    a.stats = stats;
+    a.eps = eps;
+    a.partial = static_cast<float2 *>(workspace);
+    return silu ? forward<T, true>(a, stream) : forward<T, false>(a, stream);
+}
+
+template <typename T>
+hipError_t backward_of(const void *x, const void *weight, const void *bias, const float *stats, const void *d_out, void *dx, void *d_weight, void *d_bias,
+                       const Plan &p, bool silu, void *workspace, hipStream_t stream)
+{
+    NormArgs<T> a = {};
+    a.p = p;
+    a.x = static_cast<const T *>(x);
+    a.weight = static_cast<const T *>(weight);
+    a.bias = static_cast<const T *>(bias);
+    a.in_stats = stats;
+    a.d_out = static_cast<const T *>(d_out);
+    a.out = static_cast<T *>(dx);
+    a.d_weight = static_cast<T *>(d_weight);
+    a.d_bias = static_cast<T *>(d_bias);
+    a.partial = static_cast<float2 *>(workspace);
+    a.channel = a.partial + round256(size_t(p.B) * p.strips * p.G * sizeof(float2)) / sizeof(float2);
+    return silu ? backward<T, true>(a, stream) : backward<T, false>(a, stream);
+}
+
+}  // namespace
+
+size_t group_norm_workspace_bytes(int B, int L, int C, int groups, bool is_bf16)
+{
+    const Plan p = plan_of(B, L, C, groups, is_bf16);
+    if (group_in_registers(p, is_bf16 ? 8 : 4)) return 0;
+    return round256(size_t(B) * p.strips * groups * sizeof(float2));
+}
+
+size_t group_norm_bwd_workspace_bytes(int B, int L, int C, int groups, bool is_bf16)
+{
+    const Plan p = plan_of(B, L, C, groups, is_bf16);
+    return round256(size_t(B) * p.strips * groups * sizeof(float2)) + round256(size_t(B) * p.strips * C * sizeof(float2));
+}
+
+hipError_t group_norm_launch(const void *x, const void *weight, const void *bias, void *out, float *stats, int B, int L, int C, int groups, float eps,
+                             bool silu, bool is_bf16, void *workspace, hipStream_t stream)
+{
+    const Plan p = plan_of(B, L, C, groups, is_bf16);
+    return is_bf16 ? forward_of<bf16_t>(x, weight, bias, out, stats, p, eps, silu, workspace, stream)
+                   : forward_of<float>(x, weight, bias, out, stats, p, eps, silu, workspace, stream);
+}
+
+hipError_t group_norm_bwd_launch(const void *x, const void *weight, const void *bias, const float *stats, const void *d_out, void *dx, void *d_weight,
+                                 void *d_bias, int B, int L, int C, int groups, bool silu, bool is_bf16, void *workspace, hipStream_t stream)
+{
+    const Plan p = plan_of(B, L, C, groups, is_bf16);
+    return is_bf16 ? backward_of<bf16_t>(x, weight, bias, stats, d_out, dx, d_weight, d_bias, p, silu, workspace, stream)
+                   : backward_of<float>(x, weight, bias, stats, d_out, dx, d_weight, d_bias, p, silu, workspace, stream);
+}
+
+}  // namespace vig

@@ -393,6 +393,149 @@ int gated_bigla_fwd(const void *x, const void *w1, const void *w2, const void *b
                                                     layout == VIG_LAYOUT_BLHD ? H : 0, lowrank, w2, bias, tau, by_name, workspace, s));
 }
 
+// ---- gated delta rule ----------------------------------------------------------------------------
+
+namespace {
+
+bool delta_width_ok(int d) { return head_dim_ok(d) || d == 128; }
+
+// What the three entry points ask of their sizes (L = 1 for the single-token one)
+int delta_shape_status(int B, int H, int Hk, int L, int dk, int dv, int dtype)
+{
+    if (B <= 0 || H <= 0 || Hk <= 0 || L <= 0 || dk <= 0 || dv <= 0) return VIG_ERR_SHAPE;
+    if (dtype != VIG_F32 && dtype != VIG_BF16) return VIG_ERR_DTYPE;
+    if (!delta_width_ok(dk) || !delta_width_ok(dv) || H % Hk != 0) return VIG_ERR_UNSUPPORTED;
+    // rows of a chunk are addressed with 32 bits, and a head's 64-token chunks and 16-column parts are workgroups; the
+    // workspace of the gradient is under 64 bytes per token and channel
+    if (!sizes_ok(B, H, L, 64L * (dk > dv ? dk : dv)) || long(H) * 128 >= (1L << 24) || L >= 0x7fffff00) return VIG_ERR_SHAPE;
+    if ((long(B) * H + 7) * ((long(L) + 63) / 64) > 0x7fffffffL || (long(B) * H + 7) * 8 > 0x7fffffffL) return VIG_ERR_SHAPE;
+    return VIG_OK;
+}
+
+bool direction_ok(int direction) { return direction == VIG_SCAN_FORWARD || direction == VIG_SCAN_BACKWARD; }
+
+}  // namespace
+
+size_t gated_delta_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, int dtype)
+{
+    if (delta_shape_status(B, H, Hk, L, dk, dv, dtype) != VIG_OK) return 0;
+    return vig::gated_delta_workspace_bytes(B, H, Hk, L, dk, dv, dtype == VIG_BF16);
+}
+
+int gated_delta_fwd(const void *q, const void *k, const void *v, const void *g, const void *beta, const void *initial_state, void *out,
+                    void *final_state, int B, int H, int Hk, int L, int dk, int dv, int dtype, int layout, int direction, void *workspace,
+                    size_t workspace_bytes, void *stream)
+{
+    if (!q || !k || !v || !g || !beta || !out) return VIG_ERR_NULL;
+    if (layout != VIG_LAYOUT_BHLD && layout != VIG_LAYOUT_BLHD) return VIG_ERR_LAYOUT;
+    if (!direction_ok(direction)) return VIG_ERR_UNSUPPORTED;
+    if (const int st = delta_shape_status(B, H, Hk, L, dk, dv, dtype)) return st;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(g) || !aligned16(beta) || !aligned16(initial_state) || !aligned16(out) ||
+        !aligned16(final_state) || !aligned16(workspace))
+        return VIG_ERR_ALIGN;
+    if (!workspace || workspace_bytes < gated_delta_workspace_bytes(B, H, Hk, L, dk, dv, dtype)) return VIG_ERR_WORKSPACE;
+    clear_stale_hip_error();
+    return hip_status(vig::gated_delta_launch(q, k, v, g, beta, static_cast<const float *>(initial_state), out, static_cast<float *>(final_state), B, H,
+                                              Hk, L, dk, dv, dtype == VIG_BF16, layout == VIG_LAYOUT_BLHD, direction == VIG_SCAN_BACKWARD, workspace,
+                                              static_cast<hipStream_t>(stream)));
+}
+
+size_t gated_delta_bwd_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, int dtype)
+{
+    if (delta_shape_status(B, H, Hk, L, dk, dv, dtype) != VIG_OK) return 0;
+    return vig::gated_delta_bwd_workspace_bytes(B, H, Hk, L, dk, dv, dtype == VIG_BF16);
+}
+
+int gated_delta_bwd(const void *q, const void *k, const void *v, const void *g, const void *beta, const void *initial_state, const void *d_out,
+                    const void *d_final_state, void *dq, void *dk, void *dv, void *dg, void *dbeta, void *d_initial_state, int B, int H, int Hk, int L,
+                    int dk_, int dv_, int dtype, int layout, int direction, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!q || !k || !v || !g || !beta || !d_out || !dq || !dk || !dv || !dg || !dbeta) return VIG_ERR_NULL;
+    if (layout != VIG_LAYOUT_BHLD && layout != VIG_LAYOUT_BLHD) return VIG_ERR_LAYOUT;
+    if (!direction_ok(direction)) return VIG_ERR_UNSUPPORTED;
+    if (const int st = delta_shape_status(B, H, Hk, L, dk_, dv_, dtype)) return st;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(g) || !aligned16(beta) || !aligned16(initial_state) || !aligned16(d_out) ||
+        !aligned16(d_final_state) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(dg) || !aligned16(dbeta) ||
+        !aligned16(d_initial_state) || !aligned16(workspace))
+        return VIG_ERR_ALIGN;
+    if (!workspace || workspace_bytes < gated_delta_bwd_workspace_bytes(B, H, Hk, L, dk_, dv_, dtype)) return VIG_ERR_WORKSPACE;
+    clear_stale_hip_error();
+    const vig::GradientPointers p = {q, k, v, g, beta, d_out, static_cast<const float *>(initial_state), static_cast<const float *>(d_final_state), dq, dk,
+                                     dv, dg, dbeta, static_cast<float *>(d_initial_state)};
+    return hip_status(vig::gated_delta_bwd_launch(p, B, H, Hk, L, dk_, dv_, dtype == VIG_BF16, layout == VIG_LAYOUT_BLHD,
+                                                  direction == VIG_SCAN_BACKWARD, workspace, static_cast<hipStream_t>(stream)));
+}
+
+int gated_delta_step(const void *q, const void *k, const void *v, const void *g, const void *beta, void *state, const int *slots, void *out, int B,
+                     int H, int Hk, int dk, int dv, int n_slots, int dtype, void *stream)
+{
+    if (!q || !k || !v || !g || !beta || !state || !out) return VIG_ERR_NULL;
+    if (n_slots <= 0 || (!slots && n_slots < B)) return VIG_ERR_SHAPE;
+    if (const int st = delta_shape_status(B, H, Hk, 1, dk, dv, dtype)) return st;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(g) || !aligned16(beta) || !aligned16(state) || !aligned16(slots) ||
+        !aligned16(out))
+        return VIG_ERR_ALIGN;
+    clear_stale_hip_error();
+    return hip_status(vig::gated_delta_step_launch(q, k, v, g, beta, static_cast<float *>(state), slots, out, B, H, Hk, n_slots, dk, dv,
+                                                   dtype == VIG_BF16, static_cast<hipStream_t>(stream)));
+}
+
+// ---- channels-last group norm ----------------------------------------------------------------------
+
+namespace {
+
+int norm_shape_status(int B, int L, int C, int groups, int act, int dtype)
+{
+    if (B <= 0 || L <= 0 || C <= 0 || groups <= 0) return VIG_ERR_SHAPE;
+    if (dtype != VIG_F32 && dtype != VIG_BF16) return VIG_ERR_DTYPE;
+    if (C % 8 != 0 || C > VIG_GROUP_NORM_MAX_CHANNELS || C % groups != 0 || (act != VIG_ACT_NONE && act != VIG_ACT_SILU)) return VIG_ERR_UNSUPPORTED;
+    // a workgroup per group, or per strip of at least four rows
+    if (!sizes_ok(B, L, C, 1) || long(B) * groups > 0x7fffffffL || long(B) * ((long(L) + 3) / 4) > 0x7fff0000L) return VIG_ERR_SHAPE;
+    return VIG_OK;
+}
+
+}  // namespace
+
+size_t group_norm_workspace_bytes(int B, int L, int C, int groups, int dtype)
+{
+    if (norm_shape_status(B, L, C, groups, VIG_ACT_NONE, dtype) != VIG_OK) return 0;
+    return vig::group_norm_workspace_bytes(B, L, C, groups, dtype == VIG_BF16);
+}
+
+int group_norm_act_fwd(const void *x, const void *weight, const void *bias, void *out, void *stats, int B, int L, int C, int groups, float eps, int act,
+                       int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!x || !out || !stats || !weight != !bias) return VIG_ERR_NULL;
+    if (const int st = norm_shape_status(B, L, C, groups, act, dtype)) return st;
+    if (!(eps > 0.f)) return VIG_ERR_SHAPE;
+    if (!aligned16(x) || !aligned16(weight) || !aligned16(bias) || !aligned16(out) || !aligned16(stats) || !aligned16(workspace)) return VIG_ERR_ALIGN;
+    const size_t need = group_norm_workspace_bytes(B, L, C, groups, dtype);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return VIG_ERR_WORKSPACE;
+    clear_stale_hip_error();
+    return hip_status(vig::group_norm_launch(x, weight, bias, out, static_cast<float *>(stats), B, L, C, groups, eps, act == VIG_ACT_SILU,
+                                             dtype == VIG_BF16, workspace, static_cast<hipStream_t>(stream)));
+}
+
+size_t group_norm_bwd_workspace_bytes(int B, int L, int C, int groups, int dtype)
+{
+    if (norm_shape_status(B, L, C, groups, VIG_ACT_NONE, dtype) != VIG_OK) return 0;
+    return vig::group_norm_bwd_workspace_bytes(B, L, C, groups, dtype == VIG_BF16);
+}
+
+int group_norm_act_bwd(const void *x, const void *weight, const void *bias, const void *stats, const void *d_out, void *dx, void *d_weight, void *d_bias,
+                       int B, int L, int C, int groups, int act, int dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!x || !stats || !d_out || !dx || !weight != !bias || !weight != !d_weight || !weight != !d_bias) return VIG_ERR_NULL;
+    if (const int st = norm_shape_status(B, L, C, groups, act, dtype)) return st;
+    if (!aligned16(x) || !aligned16(weight) || !aligned16(bias) || !aligned16(stats) || !aligned16(d_out) || !aligned16(dx) || !aligned16(d_weight) ||
+        !aligned16(d_bias) || !aligned16(workspace))
+        return VIG_ERR_ALIGN;
+    if (!workspace || workspace_bytes < group_norm_bwd_workspace_bytes(B, L, C, groups, dtype)) return VIG_ERR_WORKSPACE;
+    clear_stale_hip_error();
+    return hip_status(vig::group_norm_bwd_launch(x, weight, bias, static_cast<const float *>(stats), d_out, dx, d_weight, d_bias, B, L, C, groups,
+                                                 act == VIG_ACT_SILU, dtype == VIG_BF16, workspace, static_cast<hipStream_t>(stream)));
+}
+
 const char *vig_status_str(int status)
 {
     switch (status) {
@@ -401,8 +544,8 @@ const char *vig_status_str(int status)
         case VIG_ERR_SHAPE: return "VIG_ERR_SHAPE: a size is <= 0 or too large";
         case VIG_ERR_DTYPE: return "VIG_ERR_DTYPE: dtype is not VIG_F32 or VIG_BF16";
         case VIG_ERR_UNSUPPORTED:
-            return "VIG_ERR_UNSUPPORTED: head widths must be 16, 32 or 64 (model width a multiple of 32); plan a vig_plan "
-                   "the shape admits";
+            return "VIG_ERR_UNSUPPORTED: head widths must be 16, 32 or 64 (128 too for the gated delta rule; model width a "
+                   "multiple of 32); a plan, direction or activation of its list that the shape admits";
         case VIG_ERR_ALIGN: return "VIG_ERR_ALIGN: a pointer is not 16-byte aligned";
         case VIG_ERR_WORKSPACE: return "VIG_ERR_WORKSPACE: workspace missing or too small";
         case VIG_ERR_HIP: return "VIG_ERR_HIP: a HIP call failed (see vig_last_hip_error)";

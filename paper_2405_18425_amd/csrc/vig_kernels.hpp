@@ -76,4 +76,29 @@ hipError_t gate_producer_launch(const void *x, const void *w1, const void *w2, c
 // x W1 alone, bf16: lowrank [B][L][16]
 hipError_t gate_lowrank_launch(const void *x, const void *w1, void *lowrank, int B, int L, int D, hipStream_t stream);
 
+// ---- gated delta rule ----------------------------------------------------------------------------
+size_t gated_delta_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, bool is_bf16);
+hipError_t gated_delta_launch(const void *q, const void *k, const void *v, const void *g, const void *beta, const float *initial, void *out,
+                              float *final_state, int B, int H, int Hk, int L, int dk, int dv, bool is_bf16, bool token_major, bool reverse,
+                              void *workspace, hipStream_t stream);
+struct GradientPointers {
+    const void *q, *k, *v, *g, *beta, *d_out;
+    const float *initial, *d_final;  // may be null
+    void *dq, *dk, *dv, *dg, *dbeta;
+    float *d_initial;                // may be null
+};
+size_t gated_delta_bwd_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, bool is_bf16);
+hipError_t gated_delta_bwd_launch(const GradientPointers &p, int B, int H, int Hk, int L, int dk, int dv, bool is_bf16, bool token_major, bool reverse,
+                                  void *workspace, hipStream_t stream);
+hipError_t gated_delta_step_launch(const void *q, const void *k, const void *v, const void *g, const void *beta, float *state, const int *slots,
+                                   void *out, int B, int H, int Hk, int slots_n, int dk, int dv, bool is_bf16, hipStream_t stream);
+
+// ---- channels-last group norm with an activation ---------------------------------------------------
+size_t group_norm_workspace_bytes(int B, int L, int C, int groups, bool is_bf16);
+hipError_t group_norm_launch(const void *x, const void *weight, const void *bias, void *out, float *stats, int B, int L, int C, int groups, float eps,
+                             bool silu, bool is_bf16, void *workspace, hipStream_t stream);
+size_t group_norm_bwd_workspace_bytes(int B, int L, int C, int groups, bool is_bf16);
+hipError_t group_norm_bwd_launch(const void *x, const void *weight, const void *bias, const float *stats, const void *d_out, void *dx, void *d_weight,
+                                 void *d_bias, int B, int L, int C, int groups, bool silu, bool is_bf16, void *workspace, hipStream_t stream);
+
 }  // namespace vig

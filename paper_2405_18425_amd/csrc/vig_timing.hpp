@@ -16,7 +16,12 @@ enum KernelId {
     kKernelGateProducer = 6,
     kKernelSlab = 7,
     kKernelBackward = 8,
-    kKernelCount = 9
+    kKernelGatedDelta = 9,
+    kKernelGatedDeltaBackward = 10,
+    kKernelGatedDeltaStep = 11,
+    kKernelGroupNorm = 12,
+    kKernelGroupNormBackward = 13,
+    kKernelCount = 14
 };
 
 // Brackets one launch when timing is enabled on the calling thread.
