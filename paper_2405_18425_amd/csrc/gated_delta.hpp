@@ -123,20 +123,6 @@ __device__ __forceinline__ Frag from(const float *p)
 {
     return from<Frag>(*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4));
 }
-// eight values of an input row, 16-byte aligned
-__device__ __forceinline__ void load_row(Whole &f, const bf16_t *p) { f.v = *reinterpret_cast<const bf16x8 *>(p); }
-__device__ __forceinline__ void load_row(Full &f, const float *p)
-{
-    const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) f.v[j] = a[j], f.v[4 + j] = b[j];
-}
-__device__ __forceinline__ void clear(Whole &f) { f.v = bf16x8{}; }
-__device__ __forceinline__ void clear(Full &f)
-{
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f.v[j] = 0.f;
-}
 // eight single elements
 __device__ __forceinline__ void gather(Whole &f, const bf16_t (&x)[8])
 {
@@ -147,25 +133,87 @@ __device__ __forceinline__ void gather(Whole &f, const bf16_t (&x)[8])
 }
 __device__ __forceinline__ void gather(Full &f, const float (&x)[8]) { make(f, x); }
 
+// ---- memory ----------------------------------------------------------------------------------------
+// Every access goes through a buffer resource with a 32-bit byte offset that a lane forms once: the resource of a chunk's rows ends with
+// the sequence, so rows behind it read as zero and are not written.  kNowhere is behind every resource.
+using Rsrc = __amdgpu_buffer_rsrc_t;
+constexpr unsigned kNowhere = 0xc0000000u;
+
+__device__ __forceinline__ u32x4 load16(Rsrc r, unsigned at, unsigned base = 0) { return __builtin_amdgcn_raw_buffer_load_b128(r, at, base, 0); }
+__device__ __forceinline__ float load4(Rsrc r, unsigned at, unsigned base = 0)
+{
+    return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, at, base, 0));
+}
+__device__ __forceinline__ void store4(Rsrc r, unsigned at, float x, unsigned base = 0)
+{
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), r, at, base, 0);
+}
+template <typename T>
+__device__ __forceinline__ T load_element(Rsrc r, unsigned at);
+template <>
+__device__ __forceinline__ float load_element<float>(Rsrc r, unsigned at)
+{
+    return load4(r, at);
+}
+template <>
+__device__ __forceinline__ bf16_t load_element<bf16_t>(Rsrc r, unsigned at)
+{
+    return bf16_t{uint16_t(__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0))};
+}
+__device__ __forceinline__ float value(float x) { return x; }
+__device__ __forceinline__ float value(bf16_t x) { return __uint_as_float(uint32_t(x.bits) << 16); }
+template <typename T>
+__device__ __forceinline__ void store_element(Rsrc r, unsigned at, float x);
+template <>
+__device__ __forceinline__ void store_element<float>(Rsrc r, unsigned at, float x)
+{
+    store4(r, at, x);
+}
+template <>
+__device__ __forceinline__ void store_element<bf16_t>(Rsrc r, unsigned at, float x)
+{
+    __builtin_amdgcn_raw_buffer_store_b16(uint16_t(pack2(x, x)), r, at, 0, 0);
+}
+
+// Requests stay on their side of this: the compiler would move them to just before their use, where their latency is exposed
+__device__ __forceinline__ void requests_stay() { __builtin_amdgcn_sched_barrier(0xf); }
+
+// eight values of an input row, 16-byte aligned
+__device__ __forceinline__ void load_row(Whole &f, Rsrc r, unsigned at) { f.v = __builtin_bit_cast(bf16x8, load16(r, at)); }
+__device__ __forceinline__ void load_row(Full &f, Rsrc r, unsigned at)
+{
+    const u32x4 a = load16(r, at), b = load16(r, at + 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f.v[j] = __uint_as_float(a[j]), f.v[4 + j] = __uint_as_float(b[j]);
+}
+// eight consecutive 32-bit values
+__device__ __forceinline__ void load8(float (&x)[8], Rsrc r, unsigned at)
+{
+    const u32x4 a = load16(r, at), b = load16(r, at + 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(a[j]), x[4 + j] = __uint_as_float(b[j]);
+}
+
 // Fragments in the workspace: planes of 16 bytes a lane, a kilobyte each
 template <typename Frag>
 constexpr int planes = int(sizeof(Frag)) / 16;
 template <typename Frag>
 constexpr size_t frag_bytes = size_t(planes<Frag>) * 1024;
 template <typename Frag>
-__device__ __forceinline__ void put(unsigned char *ws, int block, int lane, const Frag &f)
+__device__ __forceinline__ void put(Rsrc ws, size_t first, int block, int lane, const Frag &f)
 {
     u32x4 w[planes<Frag>];
     __builtin_memcpy(w, &f, sizeof(f));
 #pragma unroll
-    for (int i = 0; i < planes<Frag>; ++i) *reinterpret_cast<u32x4 *>(ws + (size_t(block) * planes<Frag> + i) * 1024 + 16 * lane) = w[i];
+    for (int i = 0; i < planes<Frag>; ++i)
+        __builtin_amdgcn_raw_buffer_store_b128(w[i], ws, 16u * unsigned(lane), unsigned(first) + unsigned(block * planes<Frag> + i) * 1024u, 0);
 }
 template <typename Frag>
-__device__ __forceinline__ Frag get(const unsigned char *ws, int block, int lane)
+__device__ __forceinline__ Frag get(Rsrc ws, size_t first, int block, int lane)
 {
     u32x4 w[planes<Frag>];
 #pragma unroll
-    for (int i = 0; i < planes<Frag>; ++i) w[i] = *reinterpret_cast<const u32x4 *>(ws + (size_t(block) * planes<Frag> + i) * 1024 + 16 * lane);
+    for (int i = 0; i < planes<Frag>; ++i) w[i] = load16(ws, 16u * unsigned(lane), unsigned(first) + unsigned(block * planes<Frag> + i) * 1024u);
     Frag f;
     __builtin_memcpy(&f, w, sizeof(f));
     return f;
@@ -182,47 +230,41 @@ struct Shape {
     bool token_major, reverse;
 };
 
-// Rows of one head: element (t, c) at p[t * stride + c], t in scan order
-template <typename T>
-struct Rows {
-    T *p;
-    long stride;
-};
-template <typename T>
-__device__ __forceinline__ Rows<T> rows_of(T *all, const Shape &s, int b, int head, int heads, int width)
-{
-    const size_t L = size_t(s.L);
-    Rows<T> r;
-    r.p = s.token_major ? all + (size_t(b) * L * heads + head) * width : all + (size_t(b) * heads + head) * L * width;
-    r.stride = long(s.token_major ? heads : 1) * width;
-    if (s.reverse) {
-        r.p += (s.L - 1) * r.stride;
-        r.stride = -r.stride;
-    }
-    return r;
-}
+// Chunks are the same in both scan directions, 64 tokens from a multiple of 64 on; a backward scan takes the chunks, and the
+// tokens of a chunk, last first.  What is missing of the last chunk then comes before its tokens, with gate 0 and beta 0, which changes
+// no state.  Token i of a chunk in scan order:
+__device__ __forceinline__ int token_at(const Shape &s, int i) { return s.reverse ? kC - 1 - i : i; }
+__device__ __forceinline__ int chunk_at(const Shape &s, int step) { return s.reverse ? s.chunks - 1 - step : step; }
 
-// A fragment of the tokens' rows: channels 32 step + 8g .. + 7 of one row; channels the head does not have are zero
-template <typename T, typename In>
-__device__ __forceinline__ void row_frag(In &f, const Rows<const T> &rows, int t, int step, int g, int width)
+// bytes from one token's row to the next one's
+template <typename T>
+__device__ __forceinline__ unsigned pitch_of(const Shape &s, int heads, int width)
+{
+    return unsigned(s.token_major ? heads * width : width) * unsigned(sizeof(T));
+}
+// the rows of a chunk of one head of [B, heads, L, width] or [B, L, heads, width]
+template <typename T>
+__device__ __forceinline__ Rsrc chunk_rows(const T *all, const Shape &s, int b, int head, int heads, int width, int chunk)
+{
+    const size_t L = size_t(s.L), row = size_t(chunk) * kC;
+    const size_t first = s.token_major ? (size_t(b) * L + row) * heads + head : (size_t(b) * heads + head) * L + row;
+    const unsigned rows = unsigned(s.L - chunk * kC < kC ? s.L - chunk * kC : kC);
+    return slab_resource(all + first * width, (rows - 1) * pitch_of<T>(s, heads, width) + unsigned(width) * unsigned(sizeof(T)));
+}
+// everything from p on
+__device__ __forceinline__ Rsrc whole(const void *p) { return slab_resource(p, 0x80000000u); }
+// the rows of a chunk in a [slab][L][width] array of floats
+__device__ __forceinline__ Rsrc float_rows(const float *all, const Shape &s, size_t slab, int width, int chunk)
+{
+    const unsigned rows = unsigned(s.L - chunk * kC < kC ? s.L - chunk * kC : kC);
+    return slab_resource(all + (slab * s.L + size_t(chunk) * kC) * width, rows * unsigned(width) * 4u);
+}
+// where a lane's part of a fragment's row is: channels 32 step + 8g .. + 7 of a token; channels that the head does not have are nowhere
+template <typename T>
+__device__ __forceinline__ unsigned row_offset(unsigned pitch, int token, int step, int g, int width)
 {
     const int c = 32 * step + 8 * g;
-    if (c < width)
-        load_row(f, rows.p + t * rows.stride + c);
-    else
-        clear(f);
-}
-// A fragment of the transposed rows: one channel, tokens t0 .. t0 + 7 (no further than the last)
-template <typename T, typename In>
-__device__ __forceinline__ void column_frag(In &f, const Rows<const T> &rows, int t0, int last, int c, int width)
-{
-    T x[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int t = t0 + j < last ? t0 + j : last;
-        x[j] = c < width ? rows.p[t * rows.stride + c] : T{};
-    }
-    gather(f, x);
+    return c < width ? unsigned(token) * pitch + unsigned(c) * unsigned(sizeof(T)) : kNowhere;
 }
 
 // Gates of a chunk below this (and infinite ones) close it as well: exp(-10000) is 0.  Sums of them are 64-bit, so that what follows a

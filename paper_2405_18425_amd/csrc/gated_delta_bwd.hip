@@ -21,6 +21,13 @@ namespace {
 
 using namespace gd;
 
+__device__ __forceinline__ float wave_total(float x)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    return x;
+}
+
 template <typename T>
 struct AdjointArgs {
     Shape s;
@@ -46,148 +53,158 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a)
     unsigned slab, part;
     if (!chain_unit(blockIdx.x, unsigned(s.B) * unsigned(s.H), unsigned(s.dv) / 16, slab, part)) return;
     const int b = int(slab / unsigned(s.H)), h = int(slab - unsigned(b) * unsigned(s.H)), hk = h / (s.H / s.Hk);
-    const int col = 16 * int(part) + r, last = s.L - 1;
-    const Rows<const T> kr = rows_of(a.k, s, b, hk, s.Hk, s.dk), dor = rows_of(a.d_out, s, b, h, s.H, s.dv);
-    const Rows<T> dvr = rows_of(a.dv, s, b, h, s.H, s.dv);
-    const unsigned char *ws = a.ws + size_t(slab) * s.chunks * Ws::bytes;
-    const unsigned char *kw = a.key_ws + (size_t(b) * s.Hk + hk) * s.chunks * Kw::bytes;
+    const int col = 16 * int(part) + r;
+    const unsigned char *ws_all = a.ws + size_t(slab) * s.chunks * Ws::bytes;
+    const unsigned char *kw_all = a.key_ws + (size_t(b) * s.Hk + hk) * s.chunks * Kw::bytes;
+    const size_t state_size = size_t(s.dk) * s.dv;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+
+    const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk), value_pitch = pitch_of<T>(s, s.H, s.dv);
+    unsigned key_at[4], value_at[16], r_at[16];  // value j: token 32 (j / 8) + 8g + j % 8
+#pragma unroll
+    for (int m = 0; m < 4; ++m) key_at[m] = row_offset<T>(key_pitch, token_at(s, paired(m, r)), 0, g, s.dk);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const unsigned t = unsigned(token_at(s, 32 * (j >> 3) + 8 * g + (j & 7)));
+        value_at[j] = t * value_pitch + unsigned(col) * unsigned(sizeof(T));
+        r_at[j] = 4u * (t * unsigned(s.dv) + unsigned(col));
+    }
 
     f32x4 D[kCt];
 #pragma unroll
-    for (int ct = 0; ct < kCt; ++ct)
+    for (int ct = 0; ct < kCt; ++ct) D[ct] = zero;
+    if (a.d_final) {
+        const Rsrc from0 = slab_resource(a.d_final + slab * state_size, unsigned(state_size * 4));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = paired(ct, 4 * g + i);
-            D[ct][i] = a.d_final && c < s.dk ? a.d_final[(size_t(slab) * s.dk + c) * s.dv + col] : 0.f;
-        }
+        for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) D[ct][i] = load4(from0, state_offset(s, ct, i, g, col));
+    }
 
-    In fk[4][kKs], fkt[kCt][2], fqt[kCt][2];
-    Mid ft[kTriBlocks], fp[kTriBlocks];
+    In fk[4][kKs];
+    Mid fp[kTriBlocks];
     T dout[16];
-    Scalars sc;
     auto load_keys = [&](int chunk) __attribute__((always_inline)) {
+        const Rsrc kr = chunk_rows(a.k, s, b, hk, s.Hk, s.dk, chunk);
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
+        for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) {
-                const int t = chunk * kC + paired(m, r);
-                row_frag<T>(fk[m][ks], kr, t < last ? t : last, ks, g, s.dk);
-            }
+            for (int m = 0; m < 4; ++m) load_row(fk[m][ks], kr, key_at[m] + 32u * unsigned(ks * sizeof(T)));
     };
     auto load_d_out = [&](int chunk) __attribute__((always_inline)) {
+        const Rsrc dor = chunk_rows(a.d_out, s, b, h, s.H, s.dv, chunk);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {  // tokens 32 (j / 8) + 8g + j % 8: nothing comes from behind the last
-            const int t = chunk * kC + 32 * (j >> 3) + 8 * g + (j & 7);
-            dout[j] = t <= last ? dor.p[t * dor.stride + col] : T{};
-        }
+        for (int j = 0; j < 16; ++j) dout[j] = load_element<T>(dor, value_at[j]);
     };
-    auto load_triangles = [&](int chunk) __attribute__((always_inline)) {
-        const unsigned char *p = ws + size_t(chunk) * Ws::bytes;
+    auto load_scores = [&](int chunk) __attribute__((always_inline)) {
+        const Rsrc ws = whole(ws_all + size_t(chunk) * Ws::bytes);
 #pragma unroll
-        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid>(p + Ws::scores, i, lane);
-#pragma unroll
-        for (int i = 0; i < kTriBlocks; ++i) ft[i] = get<Mid>(p + Ws::inverse + kTriBlocks * frag_bytes<Mid>, i, lane);
+        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid>(ws, Ws::scores, i, lane);
     };
-    auto load_transposed = [&](int chunk) __attribute__((always_inline)) {
-        const unsigned char *p = kw + size_t(chunk) * Kw::bytes;
+    load_keys(chunk_at(s, s.chunks - 1));
+    load_d_out(chunk_at(s, s.chunks - 1));
+    load_scores(chunk_at(s, s.chunks - 1));
+    Scalars sc = load_scalars(whole(ws_all + size_t(chunk_at(s, s.chunks - 1)) * Ws::bytes), g);
+
+    for (int step = s.chunks - 1; step >= 0; --step) {
+        const int chunk = chunk_at(s, step), next = step > 0 ? chunk_at(s, step - 1) : chunk;
+        const Rsrc ws = whole(ws_all + size_t(chunk) * Ws::bytes), kw = whole(kw_all + size_t(chunk) * Kw::bytes);
+        Mid ft[kTriBlocks];
+        In fkt[kCt][2], fqt[kCt][2];
+#pragma unroll
+        for (int i = 0; i < kTriBlocks; ++i) ft[i] = get<Mid>(ws, Ws::inverse + kTriBlocks * frag_bytes<Mid>, i, lane);
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                fkt[ct][ks] = get<In>(p, 2 * ct + ks, lane);
-                fqt[ct][ks] = get<In>(p + Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
+                fkt[ct][ks] = get<In>(kw, 0, 2 * ct + ks, lane);
+                fqt[ct][ks] = get<In>(kw, Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
             }
-    };
-    load_keys(s.chunks - 1);
-    load_d_out(s.chunks - 1);
-    load_triangles(s.chunks - 1);
-    sc = load_scalars(ws + size_t(s.chunks - 1) * Ws::bytes, g);
-    load_transposed(s.chunks - 1);
-
-    for (int chunk = s.chunks - 1; chunk >= 0; --chunk) {
-        const int next = chunk > 0 ? chunk - 1 : 0;
-        float *to = a.adjoints + (size_t(slab) * s.chunks + chunk) * s.dk * s.dv + col;
+        requests_stay();
+        const Rsrc to = slab_resource(a.adjoints + (size_t(slab) * s.chunks + chunk) * state_size, unsigned(state_size * 4));
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = paired(ct, 4 * g + i);
-                if (c < s.dk) to[size_t(c) * s.dv] = D[ct][i];
-            }
+            for (int i = 0; i < 4; ++i) store4(to, state_offset(s, ct, i, g, col), D[ct][i]);
         Mid fd[kKs];
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) fd[ks] = from<Mid>(D[2 * ks], D[2 * ks + 1]);
         In fo[2];
-        f32x4 od[4];
+        Mid fod[2];
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
             T x[8];
+            float y[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] = dout[8 * p + j];
-                od[2 * p + (j >> 2)][j & 3] = io<T>::load(&x[j]) * sc.c[2 * p + (j >> 2)][j & 3];
-            }
+            for (int j = 0; j < 8; ++j) x[j] = dout[8 * p + j], y[j] = value(x[j]) * sc.c[2 * p + (j >> 2)][j & 3];
             gather(fo[p], x);
+            make(fod[p], y);
         }
         load_d_out(next);
+        requests_stay();
         f32x4 u[4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            u[m] = zero;
+        for (int m = 0; m < 4; ++m) u[m] = zero;
 #pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) mma(u[m], fk[m][ks], fd[ks]);
-            u[m] *= sc.d[m];
+        for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
-            for (int ks = m >> 1; ks < 2; ++ks) mma(u[m], fp[upper_block(m, ks)], fo[ks]);
-            u[m] *= sc.beta[m];
-        }
+            for (int m = 0; m < 4; ++m) mma(u[m], fk[m][ks], fd[ks]);
         load_keys(next);
+        requests_stay();
+#pragma unroll
+        for (int m = 0; m < 4; ++m) u[m] *= sc.d[m];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int m = 0; m <= 2 * ks + 1; ++m) mma(u[m], fp[upper_block(m, ks)], fo[ks]);
+        load_scores(next);
+        requests_stay();
+#pragma unroll
+        for (int m = 0; m < 4; ++m) u[m] *= sc.beta[m];
         const Mid fu[2] = {from<Mid>(u[0], u[1]), from<Mid>(u[2], u[3])};
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            u[m] = zero;
+        for (int m = 0; m < 4; ++m) u[m] = zero;
 #pragma unroll
-            for (int ks = m >> 1; ks < 2; ++ks) mma(u[m], ft[upper_block(m, ks)], fu[ks]);
-        }
-        load_triangles(next);
-        float *rt = a.r + size_t(slab) * s.L * s.dv + col;
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int m = 0; m <= 2 * ks + 1; ++m) mma(u[m], ft[upper_block(m, ks)], fu[ks]);
+        const Rsrc dvr = chunk_rows(a.dv, s, b, h, s.H, s.dv, chunk), rt = float_rows(a.r, s, slab, s.dv, chunk);
+        // accumulator (m, i) is token 32 (m / 2) + 8g + 4 (m % 2) + i, value 4m + i
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int t = chunk * kC + paired(m, 4 * g + i);
-                if (t <= last) {
-                    io<T>::store(dvr.p + t * dvr.stride + col, fabsf(sc.beta[m][i]) > 1e-20f ? u[m][i] : 0.f);
-                    rt[size_t(t) * s.dv] = u[m][i] / sc.beta[m][i];
-                }
-                u[m][i] *= -sc.c[m][i];
+                const float w = u[m][i];
+                store_element<T>(dvr, value_at[4 * m + i], fabsf(sc.beta[m][i]) > 1e-20f ? w : 0.f);
+                store4(rt, r_at[4 * m + i], w / sc.beta[m][i]);
+                u[m][i] = w * -sc.c[m][i];
             }
-        const Mid fw[2] = {from<Mid>(u[0], u[1]), from<Mid>(u[2], u[3])}, fod[2] = {from<Mid>(od[0], od[1]), from<Mid>(od[2], od[3])};
+        const float whole_decay = sc.whole;
+        sc = load_scalars(whole(ws_all + size_t(next) * Ws::bytes), g);
+        requests_stay();
+        const Mid fw[2] = {from<Mid>(u[0], u[1]), from<Mid>(u[2], u[3])};
 #pragma unroll
-        for (int ct = 0; ct < kCt; ++ct) {
-            D[ct] *= sc.whole;
+        for (int ct = 0; ct < kCt; ++ct) D[ct] *= whole_decay;
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                mma(D[ct], fqt[ct][ks], fod[ks]);
-                mma(D[ct], fkt[ct][ks], fw[ks]);
-            }
-        }
-        load_transposed(next);
-        sc = load_scalars(ws + size_t(next) * Ws::bytes, g);
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) mma(D[ct], fqt[ct][ks], fod[ks]);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) mma(D[ct], fkt[ct][ks], fw[ks]);
     }
-    if (a.d_initial)
+    if (a.d_initial) {
+        const Rsrc to = slab_resource(a.d_initial + slab * state_size, unsigned(state_size * 4));
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = paired(ct, 4 * g + i);
-                if (c < s.dk) a.d_initial[(size_t(slab) * s.dk + c) * s.dv + col] = D[ct][i];
-            }
+            for (int i = 0; i < 4; ++i) store4(to, state_offset(s, ct, i, g, col), D[ct][i]);
+    }
 }
 
 template <typename T, int DK, int N>
-__global__ __launch_bounds__(64) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(1, 1))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
 {
     if (blockIdx.y == 0)
         states<T, DK, N, true>(c);
@@ -204,44 +221,73 @@ struct GradientArgs {
     const unsigned char *key_ws;
 };
 
-// eight 32-bit values of a row whose columns from `width` on are zero
-__device__ __forceinline__ void row8(float (&x)[8], const float *row, int c, int width)
+// the tokens 4g .. 4g + 3 of the four-token groups of strip w in the lanes of a transposed fragment: channel r
+__device__ __forceinline__ f32x4 four_tokens(const Whole &, Rsrc keys, size_t first, int block, int w, int r, int g)
 {
-    f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-    if (c < width) lo = *reinterpret_cast<const f32x4 *>(row + c), hi = *reinterpret_cast<const f32x4 *>(row + c + 4);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = lo[j], x[4 + j] = hi[j];
+    const unsigned lane = unsigned(r + 16 * (2 * (w & 1) + (g >> 1)));
+    const u32x2 u = __builtin_amdgcn_raw_buffer_load_b64(keys, 16u * lane + 8u * unsigned(g & 1), unsigned(first) + unsigned(block) * 1024u, 0);
+    return unpack4(make_uint2(u[0], u[1]));
+}
+__device__ __forceinline__ f32x4 four_tokens(const Full &, Rsrc keys, size_t first, int block, int w, int r, int g)
+{
+    const unsigned lane = unsigned(r + 16 * (2 * (w & 1) + (g >> 1)));
+    return as_floats(load16(keys, 16u * lane + 1024u * unsigned(g & 1), unsigned(first) + unsigned(block) * 2048u));
 }
 
-// sum over the 16 lanes of a row, in its lane 15
-__device__ __forceinline__ float row_sum(float x) { return row_scan<0>(x); }
+// fragments in LDS, planes of 16 bytes a lane
+template <typename Frag>
+__device__ __forceinline__ void lds_put(unsigned char *lds, int block, int lane, const Frag &f)
+{
+    u32x4 w[planes<Frag>];
+    __builtin_memcpy(w, &f, sizeof(f));
+#pragma unroll
+    for (int i = 0; i < planes<Frag>; ++i) *reinterpret_cast<u32x4 *>(lds + (block * planes<Frag> + i) * 1024 + 16 * lane) = w[i];
+}
+template <typename Frag>
+__device__ __forceinline__ Frag lds_get(const unsigned char *lds, int block, int lane)
+{
+    u32x4 w[planes<Frag>];
+#pragma unroll
+    for (int i = 0; i < planes<Frag>; ++i) w[i] = *reinterpret_cast<const u32x4 *>(lds + (block * planes<Frag> + i) * 1024 + 16 * lane);
+    Frag f;
+    __builtin_memcpy(&f, w, sizeof(f));
+    return f;
+}
 
-// One chunk of one key head and all value heads that share it, four waves, 16 tokens each
-template <typename T, int DK, int DV>
-__global__ __launch_bounds__(256) void gd_gradients(GradientArgs<T> a)
+// One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  The contractions over value columns take kSlice of them
+// at a time: e and the rows of S and D, which all waves need, are split once and shared through LDS; afterwards X and Y take the states' place.
+template <typename T, int DK>
+__global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientArgs<T> a)
 {
     using In = typename operands<T, 2>::In;
     using Mid = typename operands<T, 2>::Mid;
     using Kw = KeyWs<T, DK, true>;
-    constexpr int kKs = DK / 32, kCt = DK / 16, kVs = DV / 32;
-    __shared__ __align__(16) float X[kC * kPitch], Y[kC * kPitch];
+    constexpr int kKs = DK / 32, kCt = DK / 16, kSlice = DK <= 64 ? 64 : 32, kVs = kSlice / 32;
+    constexpr int kStates = 2 * kCt * kVs * int(frag_bytes<Mid>), kTiles = 2 * kC * kPitch * 4;
+    __shared__ __align__(16) unsigned char shared[kStates > kTiles ? kStates : kTiles], wrong[4 * kVs * frag_bytes<Mid>];
     __shared__ double sum[kC];
     __shared__ float bet[kC], enters[kC], leaves[kC], pairs[4][kC], through[4];
+    float *X = reinterpret_cast<float *>(shared), *Y = X + kC * kPitch;
+    unsigned char *fS = shared, *fD = shared + kStates / 2;
     const Shape &s = a.s;
     const int w = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const unsigned unit = blockIdx.x, key_slab = unit / unsigned(s.chunks), chunk = unit - key_slab * unsigned(s.chunks);
+    const unsigned unit = blockIdx.x, key_slab = unit / unsigned(s.chunks);
+    const int chunk = int(unit - key_slab * unsigned(s.chunks));
     const int b = int(key_slab / unsigned(s.Hk)), hk = int(key_slab - unsigned(b) * unsigned(s.Hk)), share = s.H / s.Hk;
-    const int t0 = int(chunk) * kC, last = s.L - 1;
-    const Rows<const T> qr = rows_of(a.q, s, b, hk, s.Hk, s.dk), kr = rows_of(a.k, s, b, hk, s.Hk, s.dk);
+    const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk);
+    const Rsrc kw = whole(a.key_ws + size_t(unit) * Kw::bytes);
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    auto row = [&](int t) __attribute__((always_inline)) { return t0 + t < last ? t0 + t : last; };
-    const unsigned char *kw = a.key_ws + size_t(unit) * Kw::bytes;
 
     f32x4 qk[4], kk[4], dq[kCt], dk[kCt];
     {
+        const Rsrc qr = chunk_rows(a.q, s, b, hk, s.Hk, s.dk, chunk), kr = chunk_rows(a.k, s, b, hk, s.Hk, s.dk, chunk);
         In fq[kKs], fk[kKs];
 #pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) row_frag<T>(fq[ks], qr, row(16 * w + r), ks, g, s.dk), row_frag<T>(fk[ks], kr, row(16 * w + r), ks, g, s.dk);
+        for (int ks = 0; ks < kKs; ++ks) {
+            const unsigned at = row_offset<T>(key_pitch, token_at(s, 16 * w + r), ks, g, s.dk);
+            load_row(fq[ks], qr, at);
+            load_row(fk[ks], kr, at);
+        }
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             qk[n] = kk[n] = zero;
@@ -249,7 +295,7 @@ __global__ __launch_bounds__(256) void gd_gradients(GradientArgs<T> a)
 #pragma unroll
             for (int ks = 0; ks < kKs; ++ks) {
                 In fb;
-                row_frag<T>(fb, kr, row(16 * n + r), ks, g, s.dk);
+                load_row(fb, kr, row_offset<T>(key_pitch, token_at(s, 16 * n + r), ks, g, s.dk));
                 mma(qk[n], fq[ks], fb);
                 mma(kk[n], fk[ks], fb);
             }
@@ -259,186 +305,184 @@ __global__ __launch_bounds__(256) void gd_gradients(GradientArgs<T> a)
     for (int ct = 0; ct < kCt; ++ct) dq[ct] = dk[ct] = zero;
 
     for (int h = hk * share; h < (hk + 1) * share; ++h) {
-        const size_t slab = size_t(b) * s.H + h;
-        const Rows<const T> dor = rows_of(a.d_out, s, b, h, s.H, s.dv);
-        const float *S = a.states + (slab * s.chunks + chunk) * s.dk * s.dv, *D = a.adjoints + (slab * s.chunks + chunk) * s.dk * s.dv;
-        const float *e = a.wrong + slab * s.L * s.dv, *rr = a.r + slab * s.L * s.dv;
+        const size_t slab = size_t(b) * s.H + h, state_size = size_t(s.dk) * s.dv, state_at = (slab * s.chunks + unsigned(chunk)) * state_size;
+        const Rsrc dor = chunk_rows(a.d_out, s, b, h, s.H, s.dv, chunk), er = float_rows(a.wrong, s, slab, s.dv, chunk),
+                   rr = float_rows(a.r, s, slab, s.dv, chunk), Sr = slab_resource(a.states + state_at, unsigned(state_size * 4)),
+                   Dr = slab_resource(a.adjoints + state_at, unsigned(state_size * 4));
+        const unsigned own = unsigned(token_at(s, 16 * w + r));
         if (w == 0) {
-            const Rows<const T> gr = rows_of(a.g, s, b, h, s.H, 1), br = rows_of(a.beta, s, b, h, s.H, 1);
-            const bool there = t0 + lane <= last;
-            sum[lane] = wave_prefix(there ? double(fmaxf(io<T>::load(gr.p + row(lane) * gr.stride), kGateFloor)) : 0.0, lane);
-            bet[lane] = there ? beta_divisor(io<T>::load(br.p + row(lane) * br.stride)) : 0.f;
+            const Rsrc gr = chunk_rows(a.g, s, b, h, s.H, 1, chunk), br = chunk_rows(a.beta, s, b, h, s.H, 1, chunk);
+            const unsigned at = unsigned(token_at(s, lane)) * pitch_of<T>(s, s.H, 1);
+            sum[lane] = wave_prefix(double(fmaxf(value(load_element<T>(gr, at)), kGateFloor)), lane);
+            bet[lane] = beta_divisor(value(load_element<T>(br, at)));
         }
-        // operands of the wave's tokens; dbeta
-        In fo[kVs];
-        Mid fr[kVs], fe[kVs];
-        float db = 0.f;
+        f32x4 x[4], y[4], read[kCt], erase[kCt], write[kCt];
 #pragma unroll
-        for (int ks = 0; ks < kVs; ++ks) {
-            row_frag<T>(fo[ks], dor, row(16 * w + r), ks, g, s.dv);
-            float x[8], y[8];
-            row8(x, e + size_t(row(16 * w + r)) * s.dv, 32 * ks + 8 * g, s.dv);
-            row8(y, rr + size_t(row(16 * w + r)) * s.dv, 32 * ks + 8 * g, s.dv);
-            make(fe[ks], x);
-            make(fr[ks], y);
+        for (int n = 0; n < 4; ++n) x[n] = y[n] = zero;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) db = fmaf(x[j], y[j], db);
+        for (int ct = 0; ct < kCt; ++ct) read[ct] = erase[ct] = write[ct] = zero;
+        float db = 0.f, ds = 0.f;  // dbeta, <D, S>
+        for (int v0 = 0; v0 < s.dv; v0 += kSlice) {
+            In fo[kVs];
+            Mid fr[kVs], fe[kVs];
+#pragma unroll
+            for (int ks = 0; ks < kVs; ++ks) {
+                const int c = v0 + 32 * ks + 8 * g;
+                const bool has = c < s.dv;
+                load_row(fo[ks], dor, has ? own * pitch_of<T>(s, s.H, s.dv) + unsigned(c) * unsigned(sizeof(T)) : kNowhere);
+                const unsigned at = has ? 4u * (own * unsigned(s.dv) + unsigned(c)) : kNowhere;
+                float e8[8], r8[8];
+                load8(e8, er, at);
+                load8(r8, rr, at);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) db = fmaf(e8[j], r8[j], db);
+                make(fe[ks], e8);
+                make(fr[ks], r8);
+                lds_put(wrong, w * kVs + ks, lane, fe[ks]);
+            }
+#pragma unroll
+            for (int o = 0; o < (kCt * kVs + 3) / 4; ++o) {
+                const int block = 4 * o + w, ct = block / kVs, ks = block % kVs;
+                if (kCt * kVs % 4 != 0 && block >= kCt * kVs) break;
+                const int channel = paired(ct, r), c = v0 + 32 * ks + 8 * g;
+                const unsigned at = channel < s.dk && c < s.dv ? 4u * (unsigned(channel) * unsigned(s.dv) + unsigned(c)) : kNowhere;
+                float s8[8], d8[8];
+                load8(s8, Sr, at);
+                load8(d8, Dr, at);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) ds = fmaf(s8[j], d8[j], ds);
+                Mid f;
+                make(f, s8);
+                lds_put(fS, block, lane, f);
+                make(f, d8);
+                lds_put(fD, block, lane, f);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int ks = 0; ks < kVs; ++ks) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+                    if (n <= w) {
+                        const Mid f = n == w ? fe[ks] : lds_get<Mid>(wrong, n * kVs + ks, lane);
+                        mma(x[n], fo[ks], f);
+                        mma(y[n], fr[ks], f);
+                    }
+#pragma unroll
+                for (int ct = 0; ct < kCt; ++ct) {
+                    const Mid f = lds_get<Mid>(fS, ct * kVs + ks, lane);
+                    mma(read[ct], fo[ks], f);
+                    mma(erase[ct], fr[ks], f);
+                    mma(write[ct], fe[ks], lds_get<Mid>(fD, ct * kVs + ks, lane));
+                }
+            }
+            __syncthreads();
         }
         db += __shfl_xor(db, 16);
         db += __shfl_xor(db, 32);
-        if (g == 0 && t0 + 16 * w + r <= last) {
-            const Rows<T> dbr = rows_of(a.dbeta, s, b, h, s.H, 1);
-            io<T>::store(dbr.p + (t0 + 16 * w + r) * dbr.stride, db);
-        }
-        // <D, S>
-        float ds = 0.f;
-        for (int i = 4 * int(threadIdx.x); i < s.dk * s.dv; i += 1024) {
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(S + i), y = *reinterpret_cast<const f32x4 *>(D + i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) ds = fmaf(x[j], y[j], ds);
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) ds += __shfl_xor(ds, d);
+        if (g == 0) store_element<T>(chunk_rows(a.dbeta, s, b, h, s.H, 1, chunk), own * pitch_of<T>(s, s.H, 1), db);
+        ds = wave_total(ds);
         if (lane == 0) through[w] = ds;
-        __syncthreads();
 
         // X, Y and the pairs' part of dg
         float carry[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-            f32x4 x = zero, y = zero;
-            if (n <= w) {
-#pragma unroll
-                for (int ks = 0; ks < kVs; ++ks) {
-                    float v[8];
-                    row8(v, e + size_t(row(16 * n + r)) * s.dv, 32 * ks + 8 * g, s.dv);
-                    Mid fn;
-                    make(fn, v);
-                    mma(x, fo[ks], fn);
-                    mma(y, fr[ks], fn);
-                }
-            }
             float column = 0.f;
             const int c = 16 * n + r;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int t = 16 * w + 4 * g + i;
-                const bool in = c <= t && t0 + t <= last;
-                const float decay = in ? expf(float(sum[t] - sum[c])) * bet[c] : 0.f;
-                const float xi = in ? decay * x[i] : 0.f, yi = in && c < t ? -decay * bet[t] * y[i] : 0.f;
-                X[t * kPitch + c] = xi;
-                Y[t * kPitch + c] = yi;
+                float xi = 0.f, yi = 0.f;
                 if (n <= w) {
+                    const float decay = c <= t ? expf(float(sum[t] - sum[c])) * bet[c] : 0.f;
+                    xi = decay * x[n][i];
+                    yi = c < t ? -decay * bet[t] * y[n][i] : 0.f;
                     const float z = c < t ? xi * qk[n][i] + yi * kk[n][i] : 0.f, upto = row_scan<0>(z);
                     column += c <= t ? upto - z + carry[i] : 0.f;  // pairs (t, i < c)
                     carry[i] += __shfl(upto, lane | 15);
                 }
+                X[t * kPitch + c] = xi;
+                Y[t * kPitch + c] = yi;
             }
             column += __shfl_xor(column, 16);
             column += __shfl_xor(column, 32);
             if (g == 0) pairs[w][c] = column;
         }
-        __syncthreads();
-
-        Mid fx[2], fxt[2], fy[2];
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            const int t = 16 * w + r, c = 32 * ks + 8 * g;
-            float x[8], xt[8], y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] = X[t * kPitch + c + j];
-                xt[j] = X[(c + j) * kPitch + t];
-                y[j] = Y[t * kPitch + c + j] + Y[(c + j) * kPitch + t];
-            }
-            make(fx[ks], x);
-            make(fxt[ks], xt);
-            make(fy[ks], y);
-        }
-        f32x4 read, erase, write;  // factors of the three products with the states, by token
+        f32x4 enter = zero, leave = zero;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * w + 4 * g + i;
-            const float c = expf(float(sum[t])), d = expf(float(sum[kC - 1] - sum[t]));
-            const bool in = t0 + t <= last;
-            read[i] = in ? c : 0.f;
-            erase[i] = in ? -c * bet[t] : 0.f;
-            write[i] = in ? d * bet[t] : 0.f;
+            const float c = expf(float(sum[t])), d = expf(float(sum[kC - 1] - sum[t])) * bet[t];
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) {
+                read[ct][i] *= c;
+                erase[ct][i] *= -c * bet[t];
+                write[ct][i] *= d;
+            }
         }
-        f32x4 enter = zero, leave = zero;
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) {
-            const int c = paired(ct, r);
-            const bool has = c < s.dk;
-            f32x4 x = zero, y = zero, z = zero;
-#pragma unroll
-            for (int ks = 0; ks < kVs; ++ks) {
-                float v[8];
-                Mid f;
-                row8(v, S + size_t(has ? c : 0) * s.dv, 32 * ks + 8 * g, has ? s.dv : 0);
-                make(f, v);
-                mma(x, fo[ks], f);
-                mma(y, fr[ks], f);
-                row8(v, D + size_t(has ? c : 0) * s.dv, 32 * ks + 8 * g, has ? s.dv : 0);
-                make(f, v);
-                mma(z, fe[ks], f);
-            }
-            x *= read;
-            y *= erase;
-            z *= write;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = row(16 * w + 4 * g + i);
-                const float qe = has ? io<T>::load(qr.p + t * qr.stride + c) : 0.f, ke = has ? io<T>::load(kr.p + t * kr.stride + c) : 0.f;
-                enter[i] = fmaf(qe, x[i], fmaf(ke, y[i], enter[i]));
-                leave[i] = fmaf(ke, z[i], leave[i]);
-            }
-            dq[ct] += x;
-            dk[ct] += y + z;
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                const In fkt = get<In>(kw, 2 * ct + ks, lane), fqt = get<In>(kw + Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
-                mma(dq[ct], fx[ks], fkt);
-                mma(dk[ct], fxt[ks], fqt);
-                mma(dk[ct], fy[ks], fkt);
-            }
+            const f32x4 qe = four_tokens(In{}, kw, Kw::blocks * frag_bytes<In>, 2 * ct + (w >> 1), w, r, g);
+            const f32x4 ke = four_tokens(In{}, kw, 0, 2 * ct + (w >> 1), w, r, g);
+            enter += qe * read[ct] + ke * erase[ct];
+            leave += ke * write[ct];
+            dq[ct] += read[ct];
+            dk[ct] += erase[ct] + write[ct];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float en = row_sum(enter[i]), le = row_sum(leave[i]);
+            const float en = row_scan<0>(enter[i]), le = row_scan<0>(leave[i]);  // sums in lane 15
             if (r == 15) enters[16 * w + 4 * g + i] = en, leaves[16 * w + 4 * g + i] = le;
         }
         __syncthreads();
+
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const int t = 16 * w + r, c = 32 * ks + 8 * g;
+            float x8[8], t8[8], y8[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                x8[j] = X[t * kPitch + c + j];
+                t8[j] = X[(c + j) * kPitch + t];
+                y8[j] = Y[t * kPitch + c + j] + Y[(c + j) * kPitch + t];
+            }
+            Mid fx, ft, fy;
+            make(fx, x8);
+            make(ft, t8);
+            make(fy, y8);
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) {
+                const In fkt = get<In>(kw, 0, 2 * ct + ks, lane), fqt = get<In>(kw, Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
+                mma(dq[ct], fx, fkt);
+                mma(dk[ct], ft, fqt);
+                mma(dk[ct], fy, fkt);
+            }
+        }
         if (w == 0) {
             float after = enters[lane], before = leaves[lane];
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
-                const float x = __shfl_down(after, d), y = __shfl_up(before, d);
-                after += lane + d < 64 ? x : 0.f;
-                before += lane >= d ? y : 0.f;
+                const float u = __shfl_down(after, d), v = __shfl_up(before, d);
+                after += lane + d < 64 ? u : 0.f;
+                before += lane >= d ? v : 0.f;
             }
             const float earlier = __shfl_up(before, 1);
             before = lane > 0 ? earlier : 0.f;
             const float state = expf(float(sum[kC - 1])) * ((through[0] + through[1]) + (through[2] + through[3]));
             const float dg = after + before + ((pairs[0][lane] + pairs[1][lane]) + (pairs[2][lane] + pairs[3][lane])) + state;
-            if (t0 + lane <= last) {
-                const Rows<T> dgr = rows_of(a.dg, s, b, h, s.H, 1);
-                io<T>::store(dgr.p + (t0 + lane) * dgr.stride, dg);
-            }
+            store_element<T>(chunk_rows(a.dg, s, b, h, s.H, 1, chunk), unsigned(token_at(s, lane)) * pitch_of<T>(s, s.H, 1), dg);
         }
         __syncthreads();
     }
-    const Rows<T> dqr = rows_of(a.dq, s, b, hk, s.Hk, s.dk), dkr = rows_of(a.dk, s, b, hk, s.Hk, s.dk);
+    const Rsrc dqr = chunk_rows(a.dq, s, b, hk, s.Hk, s.dk, chunk), dkr = chunk_rows(a.dk, s, b, hk, s.Hk, s.dk, chunk);
 #pragma unroll
     for (int ct = 0; ct < kCt; ++ct) {
         const int c = paired(ct, r);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = t0 + 16 * w + 4 * g + i;
-            if (t <= last && c < s.dk) {
-                io<T>::store(dqr.p + t * dqr.stride + c, dq[ct][i]);
-                io<T>::store(dkr.p + t * dkr.stride + c, dk[ct][i]);
-            }
+            const unsigned at = c < s.dk ? unsigned(token_at(s, 16 * w + 4 * g + i)) * key_pitch + unsigned(c) * unsigned(sizeof(T)) : kNowhere;
+            store_element<T>(dqr, at, dq[ct][i]);
+            store_element<T>(dkr, at, dk[ct][i]);
         }
     }
 }
@@ -479,12 +523,7 @@ hipError_t launch(const Shape &s, const GradientPointers &p, void *workspace, hi
     gd_prepare<T, DK, N, true><<<slabs * unsigned(s.chunks), 256, 0, stream>>>(prepare);
     gd_both_chains<T, DK, N><<<dim3((slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 2), 64, 0, stream>>>(chain, adjoint);
     const unsigned key_units = unsigned(s.B) * unsigned(s.Hk) * unsigned(s.chunks);
-    if (s.dv <= 32)
-        gd_gradients<T, DK, 32><<<key_units, 256, 0, stream>>>(gradient);
-    else if (s.dv <= 64)
-        gd_gradients<T, DK, 64><<<key_units, 256, 0, stream>>>(gradient);
-    else
-        gd_gradients<T, DK, 128><<<key_units, 256, 0, stream>>>(gradient);
+    gd_gradients<T, DK><<<key_units, 256, 0, stream>>>(gradient);
     return hipGetLastError();
 }
 

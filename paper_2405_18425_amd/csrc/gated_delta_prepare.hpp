@@ -56,40 +56,40 @@ __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
     const int w = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const unsigned unit = blockIdx.x, slab = unit / unsigned(s.chunks), chunk = unit - slab * unsigned(s.chunks);
     const int b = int(slab / unsigned(s.H)), h = int(slab - unsigned(b) * unsigned(s.H)), share = s.H / s.Hk, hk = h / share;
-    const int t0 = int(chunk) * kC, last = s.L - 1;
-    const Rows<const T> kr = rows_of(a.k, s, b, hk, s.Hk, s.dk), qr = rows_of(a.q, s, b, hk, s.Hk, s.dk);
-    unsigned char *ws = a.ws + size_t(unit) * Ws::bytes;
+    const Rsrc kr = chunk_rows(a.k, s, b, hk, s.Hk, s.dk, int(chunk)), qr = chunk_rows(a.q, s, b, hk, s.Hk, s.dk, int(chunk));
+    const unsigned pitch = pitch_of<T>(s, s.Hk, s.dk);
+    const Rsrc ws = whole(a.ws + size_t(unit) * Ws::bytes);
 
     // a wave's rows of q and k; columns are the rows of the strips up to its own
     In fq[kKs], fk[kKs];
-    const int row = t0 + 16 * w + r < last ? t0 + 16 * w + r : last;
 #pragma unroll
-    for (int ks = 0; ks < kKs; ++ks) row_frag<T>(fq[ks], qr, row, ks, g, s.dk), row_frag<T>(fk[ks], kr, row, ks, g, s.dk);
+    for (int ks = 0; ks < kKs; ++ks) {
+        const unsigned at = row_offset<T>(pitch, token_at(s, 16 * w + r), ks, g, s.dk);
+        load_row(fq[ks], qr, at);
+        load_row(fk[ks], kr, at);
+    }
     if (w == 0) {
-        const Rows<const T> gr = rows_of(a.g, s, b, h, s.H, 1), br = rows_of(a.beta, s, b, h, s.H, 1);
-        const bool there = t0 + lane <= last;
-        const int t = there ? t0 + lane : last;
-        const float gate = there ? fmaxf(io<T>::load(gr.p + t * gr.stride), kGateFloor) : 0.f;
-        float beta = there ? io<T>::load(br.p + t * br.stride) : 0.f;
+        const Rsrc gr = chunk_rows(a.g, s, b, h, s.H, 1, int(chunk)), br = chunk_rows(a.beta, s, b, h, s.H, 1, int(chunk));
+        const unsigned at = unsigned(token_at(s, lane)) * pitch_of<T>(s, s.H, 1);
+        const float gate = fmaxf(value(load_element<T>(gr, at)), kGateFloor);
+        float beta = value(load_element<T>(br, at));
         if constexpr (kBwd) beta = beta_divisor(beta);
-        const double p = wave_prefix(double(gate), lane), whole = __shfl(p, 63);
+        const double p = wave_prefix(double(gate), lane), total = __shfl(p, 63);
         sum[lane] = p;
         bet[lane] = beta;
-        float *sc = reinterpret_cast<float *>(ws);
-        sc[lane] = expf(float(p));
-        sc[kC + lane] = beta;
-        sc[2 * kC + lane] = expf(float(whole - p));
+        store4(ws, 4u * unsigned(lane), expf(float(p)));
+        store4(ws, 4u * unsigned(lane), beta, 4 * kC);
+        store4(ws, 4u * unsigned(lane), expf(float(total - p)), 8 * kC);
     }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
         f32x4 kk = {0.f, 0.f, 0.f, 0.f}, qk = kk;
         if (n <= w) {
-            const int col = t0 + 16 * n + r < last ? t0 + 16 * n + r : last;
 #pragma unroll
             for (int ks = 0; ks < kKs; ++ks) {
                 In fb;
-                row_frag<T>(fb, kr, col, ks, g, s.dk);
+                load_row(fb, kr, row_offset<T>(pitch, token_at(s, 16 * n + r), ks, g, s.dk));
                 mma(kk, fk[ks], fb);
                 mma(qk, fq[ks], fb);
             }
@@ -163,33 +163,39 @@ __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
         const int c = 32 * ks + 8 * g;
-        if (ks <= (w >> 1)) put(ws + Ws::inverse, lower_block(w, ks), lane, from<Mid>(inv + tr * kPitch + c));
+        if (ks <= (w >> 1)) put(ws, Ws::inverse, lower_block(w, ks), lane, from<Mid>(inv + tr * kPitch + c));
         if constexpr (!kBwd) {
-            if (ks <= (w >> 1)) put(ws + Ws::scores, lower_block(w, ks), lane, from<MidP>(sco + tr * kPitch + c));
+            if (ks <= (w >> 1)) put(ws, Ws::scores, lower_block(w, ks), lane, from<MidP>(sco + tr * kPitch + c));
         } else if (ks >= (w >> 1)) {
             float x[8], p[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = inv[(c + j) * kPitch + tr], p[j] = sco[(c + j) * kPitch + tr];
             Mid f;
             make(f, x);
-            put(ws + Ws::inverse + kTriBlocks * frag_bytes<Mid>, upper_block(w, ks), lane, f);
+            put(ws, Ws::inverse + kTriBlocks * frag_bytes<Mid>, upper_block(w, ks), lane, f);
             make(f, p);
-            put(ws + Ws::scores, upper_block(w, ks), lane, f);
+            put(ws, Ws::scores, upper_block(w, ks), lane, f);
         }
     }
     if (h == hk * share) {  // once per key head
         using Kw = KeyWs<T, DK, kBwd>;
-        unsigned char *kw = a.key_ws + ((size_t(b) * s.Hk + hk) * s.chunks + chunk) * Kw::bytes;
+        const Rsrc kw = whole(a.key_ws + ((size_t(b) * s.Hk + hk) * s.chunks + chunk) * Kw::bytes);
 #pragma unroll
         for (int o = 0; o < Kw::blocks / 4; ++o) {
-            const int block = 4 * o + w, tile = block >> 1, ks = block & 1;
-            const int c = paired(tile, r), t = t0 + 32 * ks + 8 * g;
+            const int block = 4 * o + w, tile = block >> 1, ks = block & 1, c = paired(tile, r);
+            T x[8], y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const unsigned at = c < s.dk ? unsigned(token_at(s, 32 * ks + 8 * g + j)) * pitch + unsigned(c) * unsigned(sizeof(T)) : kNowhere;
+                x[j] = load_element<T>(kr, at);
+                if constexpr (kBwd) y[j] = load_element<T>(qr, at);
+            }
             In f;
-            column_frag<T>(f, kr, t, last, c, s.dk);
-            put(kw, block, lane, f);
+            gather(f, x);
+            put(kw, 0, block, lane, f);
             if constexpr (kBwd) {
-                column_frag<T>(f, qr, t, last, c, s.dk);
-                put(kw + Kw::blocks * frag_bytes<In>, block, lane, f);
+                gather(f, y);
+                put(kw, Kw::blocks * frag_bytes<In>, block, lane, f);
             }
         }
     }
