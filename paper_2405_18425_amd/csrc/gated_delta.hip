@@ -30,7 +30,7 @@ hipError_t launch(const Shape &s, const void *q, const void *k, const void *v, c
     const ChainArgs<T> c = {s, p.q, p.k, static_cast<const T *>(v), initial, static_cast<T *>(out), final_state, nullptr, nullptr, ws, key_ws};
     const LaunchTimer timer(kKernelGatedDelta, stream);
     gd_prepare<T, DK, N, false><<<units, 256, 0, stream>>>(p);
-    gd_states<T, DK, N><<<(slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 64, 0, stream>>>(c);
+    gd_states<T, DK, N><<<(slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 128, 0, stream>>>(c);
     return hipGetLastError();
 }
 

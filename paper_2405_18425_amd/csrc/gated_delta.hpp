@@ -175,8 +175,9 @@ __device__ __forceinline__ void store_element<bf16_t>(Rsrc r, unsigned at, float
     __builtin_amdgcn_raw_buffer_store_b16(uint16_t(pack2(x, x)), r, at, 0, 0);
 }
 
-// Requests stay on their side of this: the compiler would move them to just before their use, where their latency is exposed
-__device__ __forceinline__ void requests_stay() { __builtin_amdgcn_sched_barrier(0xf); }
+// Requests for the next chunk stand between two of these.  Left alone, the compiler moves them to just before their use, where their
+// latency is exposed, or above the last use of the registers that they are to reuse: then they get others, and a copy that waits for them.
+__device__ __forceinline__ void requests_stay() { __builtin_amdgcn_sched_barrier(0); }
 
 // eight values of an input row, 16-byte aligned
 __device__ __forceinline__ void load_row(Whole &f, Rsrc r, unsigned at) { f.v = __builtin_bit_cast(bf16x8, load16(r, at)); }
@@ -271,7 +272,7 @@ __device__ __forceinline__ unsigned row_offset(unsigned pitch, int token, int st
 // closed gate keeps its own decays.
 constexpr float kGateFloor = -10000.f;
 
-// Workspace of one chunk of one head, written by gd_prepare: c, beta, d (64 floats each, 64 spare), then fragments
+// Workspace of one chunk of one head, written by gd_prepare: c, beta, d and for the gradient 1 / beta (64 floats each), then fragments
 template <typename T, int N, bool kBwd>
 struct ChunkWs {
     using Mid = typename operands<T, N>::Mid;

@@ -41,7 +41,7 @@ struct AdjointArgs {
 
 // The chain of the adjoints for 16 value columns, one wave: the counterpart of gd::states, last chunk first
 template <typename T, int DK, int N>
-__device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a)
+__device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Columns &at, unsigned char *scal)
 {
     using In = typename operands<T, N>::In;
     using Mid = typename operands<T, N>::Mid;
@@ -49,11 +49,8 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a)
     using Kw = KeyWs<T, DK, true>;
     constexpr int kKs = DK / 32, kCt = DK / 16;
     const Shape &s = a.s;
-    const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
-    unsigned slab, part;
-    if (!chain_unit(blockIdx.x, unsigned(s.B) * unsigned(s.H), unsigned(s.dv) / 16, slab, part)) return;
-    const int b = int(slab / unsigned(s.H)), h = int(slab - unsigned(b) * unsigned(s.H)), hk = h / (s.H / s.Hk);
-    const int col = 16 * int(part) + r;
+    const int lane = at.lane, r = at.r, g = at.g, col = at.col, b = at.b, h = at.h, hk = at.hk;
+    const unsigned slab = at.slab;
     const unsigned char *ws_all = a.ws + size_t(slab) * s.chunks * Ws::bytes;
     const unsigned char *kw_all = a.key_ws + (size_t(b) * s.Hk + hk) * s.chunks * Kw::bytes;
     const size_t state_size = size_t(s.dk) * s.dv;
@@ -101,10 +98,15 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a)
 #pragma unroll
         for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid>(ws, Ws::scores, i, lane);
     };
-    load_keys(chunk_at(s, s.chunks - 1));
+    // (in the order of the loop, see gd::states)
+    u32x4 raw = request_scalars(whole(ws_all + size_t(chunk_at(s, s.chunks - 1)) * Ws::bytes), lane);
+    requests_stay();
     load_d_out(chunk_at(s, s.chunks - 1));
+    requests_stay();
+    load_keys(chunk_at(s, s.chunks - 1));
+    requests_stay();
     load_scores(chunk_at(s, s.chunks - 1));
-    Scalars sc = load_scalars(whole(ws_all + size_t(chunk_at(s, s.chunks - 1)) * Ws::bytes), g);
+    requests_stay();
 
     for (int step = s.chunks - 1; step >= 0; --step) {
         const int chunk = chunk_at(s, step), next = step > 0 ? chunk_at(s, step - 1) : chunk;
@@ -129,17 +131,23 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a)
         Mid fd[kKs];
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) fd[ks] = from<Mid>(D[2 * ks], D[2 * ks + 1]);
+        share_scalars(scal, raw, lane);
+        requests_stay();
+        raw = request_scalars(whole(ws_all + size_t(next) * Ws::bytes), lane);
+        requests_stay();
         In fo[2];
         Mid fod[2];
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
             T x[8];
             float y[8];
+            const f32x4 c[2] = {scalars(scal, kC0, 2 * p, g), scalars(scal, kC0, 2 * p + 1, g)};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = dout[8 * p + j], y[j] = value(x[j]) * sc.c[2 * p + (j >> 2)][j & 3];
+            for (int j = 0; j < 8; ++j) x[j] = dout[8 * p + j], y[j] = value(x[j]) * c[j >> 2][j & 3];
             gather(fo[p], x);
             make(fod[p], y);
         }
+        requests_stay();
         load_d_out(next);
         requests_stay();
         f32x4 u[4];
@@ -149,18 +157,20 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a)
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
             for (int m = 0; m < 4; ++m) mma(u[m], fk[m][ks], fd[ks]);
+        requests_stay();
         load_keys(next);
         requests_stay();
 #pragma unroll
-        for (int m = 0; m < 4; ++m) u[m] *= sc.d[m];
+        for (int m = 0; m < 4; ++m) u[m] *= scalars(scal, kD0, m, g);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int m = 0; m <= 2 * ks + 1; ++m) mma(u[m], fp[upper_block(m, ks)], fo[ks]);
+        requests_stay();
         load_scores(next);
         requests_stay();
 #pragma unroll
-        for (int m = 0; m < 4; ++m) u[m] *= sc.beta[m];
+        for (int m = 0; m < 4; ++m) u[m] *= scalars(scal, kBeta, m, g);
         const Mid fu[2] = {from<Mid>(u[0], u[1]), from<Mid>(u[2], u[3])};
 #pragma unroll
         for (int m = 0; m < 4; ++m) u[m] = zero;
@@ -171,20 +181,20 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a)
         const Rsrc dvr = chunk_rows(a.dv, s, b, h, s.H, s.dv, chunk), rt = float_rows(a.r, s, slab, s.dv, chunk);
         // accumulator (m, i) is token 32 (m / 2) + 8g + 4 (m % 2) + i, value 4m + i
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
+        for (int m = 0; m < 4; ++m) {
+            const f32x4 c = scalars(scal, kC0, m, g), beta = scalars(scal, kBeta, m, g), inverse = scalars(scal, kInverseBeta, m, g);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float w = u[m][i];
-                store_element<T>(dvr, value_at[4 * m + i], fabsf(sc.beta[m][i]) > 1e-20f ? w : 0.f);
-                store4(rt, r_at[4 * m + i], w / sc.beta[m][i]);
-                u[m][i] = w * -sc.c[m][i];
+                store_element<T>(dvr, value_at[4 * m + i], fabsf(beta[i]) > 1e-20f ? w : 0.f);
+                store4(rt, r_at[4 * m + i], w * inverse[i]);
+                u[m][i] = w * -c[i];
             }
-        const float whole_decay = sc.whole;
-        sc = load_scalars(whole(ws_all + size_t(next) * Ws::bytes), g);
-        requests_stay();
+        }
+        const float all = whole_decay(scal);
         const Mid fw[2] = {from<Mid>(u[0], u[1]), from<Mid>(u[2], u[3])};
 #pragma unroll
-        for (int ct = 0; ct < kCt; ++ct) D[ct] *= whole_decay;
+        for (int ct = 0; ct < kCt; ++ct) D[ct] *= all;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -206,10 +216,13 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a)
 template <typename T, int DK, int N>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(1, 1))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
 {
+    __shared__ __align__(16) unsigned char scal[kScalarBytes];
+    Columns at;
+    if (!columns_of(a.s, at)) return;
     if (blockIdx.y == 0)
-        states<T, DK, N, true>(c);
+        states<T, DK, N, true>(c, at, scal, nullptr);
     else
-        adjoint_chain<T, DK, N>(a);
+        adjoint_chain<T, DK, N>(a, at, scal);
 }
 
 template <typename T>
@@ -232,26 +245,6 @@ __device__ __forceinline__ f32x4 four_tokens(const Full &, Rsrc keys, size_t fir
 {
     const unsigned lane = unsigned(r + 16 * (2 * (w & 1) + (g >> 1)));
     return as_floats(load16(keys, 16u * lane + 1024u * unsigned(g & 1), unsigned(first) + unsigned(block) * 2048u));
-}
-
-// fragments in LDS, planes of 16 bytes a lane
-template <typename Frag>
-__device__ __forceinline__ void lds_put(unsigned char *lds, int block, int lane, const Frag &f)
-{
-    u32x4 w[planes<Frag>];
-    __builtin_memcpy(w, &f, sizeof(f));
-#pragma unroll
-    for (int i = 0; i < planes<Frag>; ++i) *reinterpret_cast<u32x4 *>(lds + (block * planes<Frag> + i) * 1024 + 16 * lane) = w[i];
-}
-template <typename Frag>
-__device__ __forceinline__ Frag lds_get(const unsigned char *lds, int block, int lane)
-{
-    u32x4 w[planes<Frag>];
-#pragma unroll
-    for (int i = 0; i < planes<Frag>; ++i) w[i] = *reinterpret_cast<const u32x4 *>(lds + (block * planes<Frag> + i) * 1024 + 16 * lane);
-    Frag f;
-    __builtin_memcpy(&f, w, sizeof(f));
-    return f;
 }
 
 // One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  The contractions over value columns take kSlice of them

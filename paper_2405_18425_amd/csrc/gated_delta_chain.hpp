@@ -1,8 +1,8 @@
-// states: the chain of a head's chunks, S -> S_out, for 16 value columns, one wave.  See gated_delta.hpp for the formulas.
+// The chain of a head's chunks, S -> S_out, for 16 value columns, one wave, and a second wave for their outputs.  Formulas: gated_delta.hpp.
 //
-// The wave holds its columns of the state in accumulators (32-bit) and takes a chunk's matrices from the workspace as fragments, 16 bytes
-// a lane: what a step needs first (K, That, V) is requested for the next chunk as soon as its last product of this chunk has been issued,
-// what it needs later at its start.  Nothing goes through LDS and there is no barrier.  Columns of one head sit on one XCD (blockIdx % 8), whose L2 they read the fragments from.
+// The chain's wave holds its columns of the state in accumulators (32-bit) and takes a chunk's matrices from the workspace as fragments, 16 bytes
+// a lane, each requested for the next chunk as soon as its last product of this chunk has been issued.  The three products of a step
+// follow each other in registers; only what the outputs need goes through LDS, with one barrier a chunk.  Columns of one head sit on one XCD (blockIdx % 8), whose L2 they read the fragments from.
 #pragma once
 
 #include "gated_delta.hpp"
@@ -42,25 +42,26 @@ __device__ __forceinline__ const Full &first_parts(const Full &f)
     return f;
 }
 
-// the three scalars of the tokens 8g .. 8g + 7 of each half chunk
-struct Scalars {
-    f32x4 c[4], beta[4], d[4];
-    float whole;
-};
 __device__ __forceinline__ f32x4 as_floats(const u32x4 &x) { return __builtin_bit_cast(f32x4, x); }
-__device__ __forceinline__ Scalars load_scalars(Rsrc ws, int g)
+
+// A chunk's scalars: a lane requests 16 bytes of the kilobyte, the wave shares them through its own LDS when the chunk's turn comes (as
+// registers of the lanes that use them they would be 37 for a whole step), and reads what it needs when it needs it.
+constexpr int kScalarBytes = 1024;
+__device__ __forceinline__ u32x4 request_scalars(Rsrc ws, int lane) { return load16(ws, 16u * unsigned(lane)); }
+__device__ __forceinline__ void share_scalars(unsigned char *lds, const u32x4 &x, int lane)
 {
-    Scalars x;
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-        const unsigned at = 32u * unsigned(g), base = 128u * unsigned(m >> 1) + 16u * unsigned(m & 1);
-        x.c[m] = as_floats(load16(ws, at, base));
-        x.beta[m] = as_floats(load16(ws, at, base + 4 * kC));
-        x.d[m] = as_floats(load16(ws, at, base + 8 * kC));
-    }
-    x.whole = load4(ws, 0, 4 * (kC - 1));
-    return x;
+    *reinterpret_cast<u32x4 *>(lds + 16 * lane) = x;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
+// of the tokens that accumulators of tile m stand for
+enum Scalar { kC0 = 0, kBeta = 256, kD0 = 512, kInverseBeta = 768 };
+__device__ __forceinline__ f32x4 scalars(const unsigned char *lds, Scalar which, int m, int g)
+{
+    return *reinterpret_cast<const f32x4 *>(lds + which + 128 * (m >> 1) + 16 * (m & 1) + 32 * g);
+}
+__device__ __forceinline__ float whole_decay(const unsigned char *lds) { return *reinterpret_cast<const float *>(lds + 4 * (kC - 1)); }
 
 // Rows of a state: element (channel, column) of [dk][dv] floats in the lanes that hold it; channels that the head does not have are nowhere
 __device__ __forceinline__ unsigned state_offset(const Shape &s, int ct, int i, int g, int col)
@@ -69,27 +70,70 @@ __device__ __forceinline__ unsigned state_offset(const Shape &s, int ct, int i, 
     return c < s.dk ? 4u * (unsigned(c) * unsigned(s.dv) + unsigned(col)) : kNowhere;
 }
 
+// What the chain of a chunk leaves for its outputs, in LDS: the state as fragments (two parts) and u as it is
+template <typename T, int DK>
+struct HandOver {
+    using Mid2 = typename operands<T, 2>::Mid;
+    static constexpr int u = DK / 32 * int(frag_bytes<Mid2>);
+    static constexpr int bytes = u + 4096;
+};
+template <typename Frag>
+__device__ __forceinline__ void lds_put(unsigned char *lds, int block, int lane, const Frag &f)
+{
+    u32x4 w[planes<Frag>];
+    __builtin_memcpy(w, &f, sizeof(f));
+#pragma unroll
+    for (int i = 0; i < planes<Frag>; ++i) *reinterpret_cast<u32x4 *>(lds + (block * planes<Frag> + i) * 1024 + 16 * lane) = w[i];
+}
+template <typename Frag>
+__device__ __forceinline__ Frag lds_get(const unsigned char *lds, int block, int lane)
+{
+    u32x4 w[planes<Frag>];
+#pragma unroll
+    for (int i = 0; i < planes<Frag>; ++i) w[i] = *reinterpret_cast<const u32x4 *>(lds + (block * planes<Frag> + i) * 1024 + 16 * lane);
+    Frag f;
+    __builtin_memcpy(&f, w, sizeof(f));
+    return f;
+}
+
+// a wave's 16 columns of one head
+struct Columns {
+    unsigned slab;
+    int b, h, hk, col, lane, r, g;
+};
+__device__ __forceinline__ bool columns_of(const Shape &s, Columns &c)
+{
+    unsigned part;
+    if (!chain_unit(blockIdx.x, unsigned(s.B) * unsigned(s.H), unsigned(s.dv) / 16, c.slab, part)) return false;
+    c.b = int(c.slab / unsigned(s.H));
+    c.h = int(c.slab - unsigned(c.b) * unsigned(s.H));
+    c.hk = c.h / (s.H / s.Hk);
+    c.lane = threadIdx.x & 63;
+    c.r = c.lane & 15;
+    c.g = c.lane >> 4;
+    c.col = 16 * int(part) + c.r;
+    return true;
+}
+
 template <typename T, int DK, int N, bool kBwd>
-__device__ __forceinline__ void states(const ChainArgs<T> &a)
+__device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at, unsigned char *scal /* the wave's scalars */,
+                                       unsigned char *lds /* two HandOvers; forward */)
 {
     using In = typename operands<T, N>::In;
     using Mid = typename operands<T, N>::Mid;
-    using Mid2 = typename operands<T, 2>::Mid;
     using Ws = ChunkWs<T, N, kBwd>;
     using Kw = KeyWs<T, DK, kBwd>;
+    using Hand = HandOver<T, DK>;
     constexpr int kKs = DK / 32, kCt = DK / 16;
     const Shape &s = a.s;
-    const int lane = threadIdx.x, r = lane & 15, g = lane >> 4;
-    unsigned slab, part;
-    if (!chain_unit(blockIdx.x, unsigned(s.B) * unsigned(s.H), unsigned(s.dv) / 16, slab, part)) return;
-    const int b = int(slab / unsigned(s.H)), h = int(slab - unsigned(b) * unsigned(s.H)), hk = h / (s.H / s.Hk);
-    const int col = 16 * int(part) + r;
+    const int lane = at.lane, r = at.r, g = at.g, col = at.col;
+    const unsigned slab = at.slab;
     const unsigned char *ws_all = a.ws + size_t(slab) * s.chunks * Ws::bytes;
-    const unsigned char *kw_all = a.key_ws + (size_t(b) * s.Hk + hk) * s.chunks * Kw::bytes;
+    const unsigned char *kw_all = a.key_ws + (size_t(at.b) * s.Hk + at.hk) * s.chunks * Kw::bytes;
     const size_t state_size = size_t(s.dk) * s.dv;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
-    // offsets of a lane's rows: of keys and queries, and of its 16 values
+    // offsets of a lane's rows: of keys, and of its 16 values
     const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk), value_pitch = pitch_of<T>(s, s.H, s.dv);
     unsigned key_at[4], value_at[16], e_at[16];
 #pragma unroll
@@ -112,19 +156,19 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a)
             for (int i = 0; i < 4; ++i) S[ct][i] = load4(from0, state_offset(s, ct, i, g, col));
     }
 
-    In fk[4][kKs];
+    In fk[4][kKs], fkt[kCt][2];
     Mid ft[kTriBlocks];
     T v[16];
     auto ws_of = [&](int chunk) __attribute__((always_inline)) { return whole(ws_all + size_t(chunk) * Ws::bytes); };
     auto load_keys = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc kr = chunk_rows(a.k, s, b, hk, s.Hk, s.dk, chunk);
+        const Rsrc kr = chunk_rows(a.k, s, at.b, at.hk, s.Hk, s.dk, chunk);
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
             for (int m = 0; m < 4; ++m) load_row(fk[m][ks], kr, key_at[m] + 32u * unsigned(ks * sizeof(T)));
     };
     auto load_values = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc vr = chunk_rows(a.v, s, b, h, s.H, s.dv, chunk);
+        const Rsrc vr = chunk_rows(a.v, s, at.b, at.h, s.H, s.dv, chunk);
 #pragma unroll
         for (int j = 0; j < 16; ++j) v[j] = load_element<T>(vr, value_at[j]);
     };
@@ -133,52 +177,62 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a)
 #pragma unroll
         for (int i = 0; i < kTriBlocks; ++i) ft[i] = get<Mid>(ws, Ws::inverse, i, lane);
     };
+    auto load_transposed = [&](int chunk) __attribute__((always_inline)) {
+        const Rsrc kw = whole(kw_all + size_t(chunk) * Kw::bytes);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) fkt[ct][ks] = get<In>(kw, 0, 2 * ct + ks, lane);
+    };
+    // (in the order of the loop: its waits count the requests behind the one they are for, and hold for the way into the loop as well)
+    u32x4 raw = request_scalars(ws_of(chunk_at(s, 0)), lane);
+    requests_stay();
     load_keys(chunk_at(s, 0));
+    requests_stay();
     load_values(chunk_at(s, 0));
+    requests_stay();
     load_inverse(chunk_at(s, 0));
-    Scalars sc = load_scalars(ws_of(chunk_at(s, 0)), g);
+    requests_stay();
+    load_transposed(chunk_at(s, 0));
+    requests_stay();
 
     for (int step = 0; step < s.chunks; ++step) {
         const int chunk = chunk_at(s, step), next = step + 1 < s.chunks ? chunk_at(s, step + 1) : chunk;
-        const Rsrc ws = ws_of(chunk), kw = whole(kw_all + size_t(chunk) * Kw::bytes);
-        In fq[4][kKs], fkt[kCt][2];
-        Mid2 fp[kTriBlocks];
-        if constexpr (!kBwd) {
-            const Rsrc qr = chunk_rows(a.q, s, b, hk, s.Hk, s.dk, chunk);
-#pragma unroll
-            for (int ks = 0; ks < kKs; ++ks)
-#pragma unroll
-                for (int m = 0; m < 4; ++m) load_row(fq[m][ks], qr, key_at[m] + 32u * unsigned(ks * sizeof(T)));
-#pragma unroll
-            for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid2>(ws, Ws::scores, i, lane);
-        } else {
+        unsigned char *hand = lds + (step & 1) * Hand::bytes;
+        if constexpr (kBwd) {
             const Rsrc to = slab_resource(a.states + (size_t(slab) * s.chunks + chunk) * state_size, unsigned(state_size * 4));
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) store4(to, state_offset(s, ct, i, g, col), S[ct][i]);
         }
-#pragma unroll
-        for (int ct = 0; ct < kCt; ++ct)
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) fkt[ct][ks] = get<In>(kw, 0, 2 * ct + ks, lane);
+        share_scalars(scal, raw, lane);
+        requests_stay();
+        raw = request_scalars(ws_of(next), lane);
         requests_stay();
         Mid fs[kKs];
 #pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) fs[ks] = from<Mid>(S[2 * ks], S[2 * ks + 1]);
-        f32x4 e[4], o[4];
+        for (int ks = 0; ks < kKs; ++ks) {
+            fs[ks] = from<Mid>(S[2 * ks], S[2 * ks + 1]);
+            if constexpr (!kBwd) lds_put(hand, ks, lane, first_parts<N, 2>(fs[ks]));
+        }
+        f32x4 e[4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) e[m] = o[m] = zero;
+        for (int m = 0; m < 4; ++m) e[m] = zero;
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
             for (int m = 0; m < 4; ++m) mma(e[m], fk[m][ks], fs[ks]);
+        requests_stay();
         load_keys(next);
         requests_stay();
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
+        for (int m = 0; m < 4; ++m) {
+            const f32x4 c = scalars(scal, kC0, m, g);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[m][i] = fmaf(-sc.c[m][i], e[m][i], value(v[4 * m + i]));
+            for (int i = 0; i < 4; ++i) e[m][i] = fmaf(-c[i], e[m][i], value(v[4 * m + i]));
+        }
+        requests_stay();
         load_values(next);
         requests_stay();
         const Mid fe[2] = {from<Mid>(e[0], e[1]), from<Mid>(e[2], e[3])};
@@ -188,46 +242,32 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a)
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int m = 2 * ks; m < 4; ++m) mma(e[m], ft[lower_block(m, ks)], fe[ks]);
+        requests_stay();
         load_inverse(next);
         requests_stay();
         if constexpr (kBwd) {
             const Rsrc to = float_rows(a.wrong, s, slab, s.dv, chunk);
 #pragma unroll
             for (int j = 0; j < 16; ++j) store4(to, e_at[j], e[j >> 2][j & 3]);
-        } else {
-#pragma unroll
-            for (int ks = 0; ks < kKs; ++ks)
-#pragma unroll
-                for (int m = 0; m < 4; ++m) mma(o[m], fq[m][ks], first_parts<N, 2>(fs[ks]));
         }
 #pragma unroll
-        for (int m = 0; m < 4; ++m) e[m] *= sc.beta[m];  // u
-        if constexpr (!kBwd) {
-            const Mid2 fu[2] = {from<Mid2>(e[0], e[1]), from<Mid2>(e[2], e[3])};
-#pragma unroll
-            for (int m = 0; m < 4; ++m) o[m] *= sc.c[m];
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-                for (int m = 2 * ks; m < 4; ++m) mma(o[m], fp[lower_block(m, ks)], fu[ks]);
+        for (int m = 0; m < 4; ++m) {
+            e[m] *= scalars(scal, kBeta, m, g);  // u
+            if constexpr (!kBwd) *reinterpret_cast<f32x4 *>(hand + Hand::u + 1024 * m + 16 * lane) = e[m];
+            e[m] *= scalars(scal, kD0, m, g);
         }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) e[m] *= sc.d[m];
-        const float whole_decay = sc.whole;
-        sc = load_scalars(ws_of(next), g);
-        requests_stay();
+        const float whole = whole_decay(scal);
         const Mid fd[2] = {from<Mid>(e[0], e[1]), from<Mid>(e[2], e[3])};
 #pragma unroll
-        for (int ct = 0; ct < kCt; ++ct) S[ct] *= whole_decay;
+        for (int ct = 0; ct < kCt; ++ct) S[ct] *= whole;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) mma(S[ct], fkt[ct][ks], fd[ks]);
-        if constexpr (!kBwd) {
-            const Rsrc to = chunk_rows(a.out, s, b, h, s.H, s.dv, chunk);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) store_element<T>(to, value_at[j], o[j >> 2][j & 3]);
-        }
+        requests_stay();
+        load_transposed(next);
+        requests_stay();
+        if constexpr (!kBwd) __syncthreads();
     }
     if (a.final_state) {
         const Rsrc to = slab_resource(a.final_state + slab * state_size, unsigned(state_size * 4));
@@ -238,10 +278,93 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a)
     }
 }
 
+// The outputs of a wave's columns, one chunk behind the chain
 template <typename T, int DK, int N>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(1, 1))) void gd_states(ChainArgs<T> a)
+__device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at, const unsigned char *lds)
 {
-    states<T, DK, N, false>(a);
+    using In = typename operands<T, N>::In;
+    using Mid2 = typename operands<T, 2>::Mid;
+    using Ws = ChunkWs<T, N, false>;
+    using Hand = HandOver<T, DK>;
+    constexpr int kKs = DK / 32;
+    const Shape &s = a.s;
+    const int lane = at.lane, r = at.r, g = at.g;
+    const unsigned char *ws_all = a.ws + size_t(at.slab) * s.chunks * Ws::bytes;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk), value_pitch = pitch_of<T>(s, s.H, s.dv);
+    unsigned key_at[4], value_at[16];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) key_at[m] = row_offset<T>(key_pitch, token_at(s, paired(m, r)), 0, g, s.dk);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) value_at[j] = unsigned(token_at(s, paired(j >> 2, 4 * g + (j & 3)))) * value_pitch + unsigned(at.col) * unsigned(sizeof(T));
+
+    In fq[4][kKs];
+    Mid2 fp[kTriBlocks];
+    f32x4 c[4];
+    auto load_queries = [&](int chunk) __attribute__((always_inline)) {
+        const Rsrc qr = chunk_rows(a.q, s, at.b, at.hk, s.Hk, s.dk, chunk);
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) load_row(fq[m][ks], qr, key_at[m] + 32u * unsigned(ks * sizeof(T)));
+    };
+    auto load_scores = [&](int chunk) __attribute__((always_inline)) {
+        const Rsrc ws = whole(ws_all + size_t(chunk) * Ws::bytes);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) c[m] = as_floats(load16(ws, 32u * unsigned(g), 128u * unsigned(m >> 1) + 16u * unsigned(m & 1)));
+#pragma unroll
+        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid2>(ws, Ws::scores, i, lane);
+    };
+    load_queries(chunk_at(s, 0));
+    requests_stay();
+    load_scores(chunk_at(s, 0));
+    requests_stay();
+    for (int step = 0; step < s.chunks; ++step) {
+        const int chunk = chunk_at(s, step), next = step + 1 < s.chunks ? chunk_at(s, step + 1) : chunk;
+        const unsigned char *hand = lds + (step & 1) * Hand::bytes;
+        __syncthreads();  // the chain has left this chunk's state and u; it writes the other half until the next one
+        f32x4 o[4], u[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            o[m] = zero;
+            u[m] = *reinterpret_cast<const f32x4 *>(hand + Hand::u + 1024 * m + 16 * lane);
+        }
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+            const Mid2 fs = lds_get<Mid2>(hand, ks, lane);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) mma(o[m], fq[m][ks], fs);
+        }
+        requests_stay();
+        load_queries(next);
+        requests_stay();
+        const Mid2 fu[2] = {from<Mid2>(u[0], u[1]), from<Mid2>(u[2], u[3])};
+#pragma unroll
+        for (int m = 0; m < 4; ++m) o[m] *= c[m];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int m = 2 * ks; m < 4; ++m) mma(o[m], fp[lower_block(m, ks)], fu[ks]);
+        requests_stay();
+        load_scores(next);
+        requests_stay();
+        const Rsrc to = chunk_rows(a.out, s, at.b, at.h, s.H, s.dv, chunk);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) store_element<T>(to, value_at[j], o[j >> 2][j & 3]);
+    }
+}
+
+// Two waves per 16 columns: the chain, and the outputs one chunk behind it
+template <typename T, int DK, int N>
+__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) void gd_states(ChainArgs<T> a)
+{
+    __shared__ __align__(16) unsigned char lds[2 * HandOver<T, DK>::bytes], scal[kScalarBytes];
+    Columns at;
+    if (!columns_of(a.s, at)) return;
+    if (threadIdx.x < 64)
+        states<T, DK, N, false>(a, at, scal, lds);
+    else
+        outputs<T, DK, N>(a, at, lds);
 }
 
 }  // namespace gd

@@ -80,6 +80,7 @@ __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
         store4(ws, 4u * unsigned(lane), expf(float(p)));
         store4(ws, 4u * unsigned(lane), beta, 4 * kC);
         store4(ws, 4u * unsigned(lane), expf(float(total - p)), 8 * kC);
+        if constexpr (kBwd) store4(ws, 4u * unsigned(lane), 1.f / beta, 12 * kC);
     }
     __syncthreads();
 #pragma unroll
