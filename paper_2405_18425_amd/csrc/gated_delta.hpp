@@ -195,6 +195,24 @@ __device__ __forceinline__ void load8(float (&x)[8], Rsrc r, unsigned at)
     for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(a[j]), x[4 + j] = __uint_as_float(b[j]);
 }
 
+// eight values of an output row
+__device__ __forceinline__ void store_row(Rsrc r, unsigned at, const float (&x)[8], bf16_t)
+{
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}, r, at, 0, 0);
+}
+__device__ __forceinline__ void store_row(Rsrc r, unsigned at, const float (&x)[8], float)
+{
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]}), r, at, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]}), r, at + 16, 0, 0);
+}
+// what the wave has put into its own part of LDS is there for its other lanes
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Fragments in the workspace: planes of 16 bytes a lane, a kilobyte each
 template <typename Frag>
 constexpr int planes = int(sizeof(Frag)) / 16;
@@ -254,12 +272,6 @@ __device__ __forceinline__ Rsrc chunk_rows(const T *all, const Shape &s, int b, 
 }
 // everything from p on
 __device__ __forceinline__ Rsrc whole(const void *p) { return slab_resource(p, 0x80000000u); }
-// the rows of a chunk in a [slab][L][width] array of floats
-__device__ __forceinline__ Rsrc float_rows(const float *all, const Shape &s, size_t slab, int width, int chunk)
-{
-    const unsigned rows = unsigned(s.L - chunk * kC < kC ? s.L - chunk * kC : kC);
-    return slab_resource(all + (slab * s.L + size_t(chunk) * kC) * width, rows * unsigned(width) * 4u);
-}
 // where a lane's part of a fragment's row is: channels 32 step + 8g .. + 7 of a token; channels that the head does not have are nowhere
 template <typename T>
 __device__ __forceinline__ unsigned row_offset(unsigned pitch, int token, int step, int g, int width)

@@ -32,124 +32,98 @@ template <typename T>
 struct AdjointArgs {
     Shape s;
     const T *k, *d_out;
-    const float *d_final;      // [B, H, dk, dv] or null
+    const float *d_final;         // [B, H, dk, dv] or null
     T *dv;
-    float *d_initial;          // [B, H, dk, dv] or null
-    float *adjoints, *r;       // D of every chunk [slab][chunk][dk][dv], r [slab][L][dv]
+    float *d_initial;             // [B, H, dk, dv] or null
+    unsigned char *adjoints, *r;  // D and r of every chunk as fragments, see gd::Tile
     const unsigned char *ws, *key_ws;
 };
 
-// The chain of the adjoints for 16 value columns, one wave: the counterpart of gd::states, last chunk first
+// The chain of the adjoints for 16 value columns, last chunk first, the counterpart of gd::states: one wave holds D and takes the three products
+// that depend on it; a second one makes what does not, P^T dO and Q^T (c . dO), a chunk ahead, and takes D, w and r away, a chunk behind.
+template <int DK>
+struct AdjointLds {
+    static constexpr int ahead = 4096 + DK * 64;                     // P^T dO, Q^T (c . dO): accumulators, 16 bytes a lane
+    static constexpr int behind = Tile<DK>::bytes + Tile<kC>::bytes;  // D, w
+    static constexpr int bytes = 2 * (ahead + behind);
+};
+
 template <typename T, int DK, int N>
-__device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Columns &at, unsigned char *scal)
+__device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Columns &at, unsigned char *scal, unsigned char *lds)
 {
     using In = typename operands<T, N>::In;
     using Mid = typename operands<T, N>::Mid;
     using Ws = ChunkWs<T, N, true>;
     using Kw = KeyWs<T, DK, true>;
+    using Lds = AdjointLds<DK>;
     constexpr int kKs = DK / 32, kCt = DK / 16;
     const Shape &s = a.s;
-    const int lane = at.lane, r = at.r, g = at.g, col = at.col, b = at.b, h = at.h, hk = at.hk;
-    const unsigned slab = at.slab;
-    const unsigned char *ws_all = a.ws + size_t(slab) * s.chunks * Ws::bytes;
-    const unsigned char *kw_all = a.key_ws + (size_t(b) * s.Hk + hk) * s.chunks * Kw::bytes;
+    const int lane = at.lane, r = at.r, g = at.g, col = at.col;
+    const unsigned char *ws_all = a.ws + size_t(at.slab) * s.chunks * Ws::bytes;
+    const unsigned char *kw_all = a.key_ws + (size_t(at.b) * s.Hk + at.hk) * s.chunks * Kw::bytes;
     const size_t state_size = size_t(s.dk) * s.dv;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-
-    const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk), value_pitch = pitch_of<T>(s, s.H, s.dv);
-    unsigned key_at[4], value_at[16], r_at[16];  // value j: token 32 (j / 8) + 8g + j % 8
+    const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk);
+    unsigned key_at[4];
 #pragma unroll
     for (int m = 0; m < 4; ++m) key_at[m] = row_offset<T>(key_pitch, token_at(s, paired(m, r)), 0, g, s.dk);
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const unsigned t = unsigned(token_at(s, 32 * (j >> 3) + 8 * g + (j & 7)));
-        value_at[j] = t * value_pitch + unsigned(col) * unsigned(sizeof(T));
-        r_at[j] = 4u * (t * unsigned(s.dv) + unsigned(col));
-    }
 
     f32x4 D[kCt];
 #pragma unroll
     for (int ct = 0; ct < kCt; ++ct) D[ct] = zero;
     if (a.d_final) {
-        const Rsrc from0 = slab_resource(a.d_final + slab * state_size, unsigned(state_size * 4));
+        const Rsrc from0 = slab_resource(a.d_final + at.slab * state_size, unsigned(state_size * 4));
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
             for (int i = 0; i < 4; ++i) D[ct][i] = load4(from0, state_offset(s, ct, i, g, col));
     }
 
-    In fk[4][kKs];
-    Mid fp[kTriBlocks];
-    T dout[16];
+    In fk[4][kKs], fkt[kCt][2];
+    Mid ft[kTriBlocks];
     auto load_keys = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc kr = chunk_rows(a.k, s, b, hk, s.Hk, s.dk, chunk);
+        const Rsrc kr = chunk_rows(a.k, s, at.b, at.hk, s.Hk, s.dk, chunk);
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
             for (int m = 0; m < 4; ++m) load_row(fk[m][ks], kr, key_at[m] + 32u * unsigned(ks * sizeof(T)));
     };
-    auto load_d_out = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc dor = chunk_rows(a.d_out, s, b, h, s.H, s.dv, chunk);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) dout[j] = load_element<T>(dor, value_at[j]);
-    };
-    auto load_scores = [&](int chunk) __attribute__((always_inline)) {
+    auto load_inverse = [&](int chunk) __attribute__((always_inline)) {
         const Rsrc ws = whole(ws_all + size_t(chunk) * Ws::bytes);
 #pragma unroll
-        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid>(ws, Ws::scores, i, lane);
+        for (int i = 0; i < kTriBlocks; ++i) ft[i] = get<Mid>(ws, Ws::inverse + kTriBlocks * frag_bytes<Mid>, i, lane);
+    };
+    auto load_transposed = [&](int chunk) __attribute__((always_inline)) {
+        const Rsrc kw = whole(kw_all + size_t(chunk) * Kw::bytes);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) fkt[ct][ks] = get<In>(kw, 0, 2 * ct + ks, lane);
     };
     // (in the order of the loop, see gd::states)
-    u32x4 raw = request_scalars(whole(ws_all + size_t(chunk_at(s, s.chunks - 1)) * Ws::bytes), lane);
+    const int first = chunk_at(s, s.chunks - 1);
+    u32x4 raw = request_scalars(whole(ws_all + size_t(first) * Ws::bytes), lane);
     requests_stay();
-    load_d_out(chunk_at(s, s.chunks - 1));
+    load_keys(first);
     requests_stay();
-    load_keys(chunk_at(s, s.chunks - 1));
+    load_inverse(first);
     requests_stay();
-    load_scores(chunk_at(s, s.chunks - 1));
+    load_transposed(first);
     requests_stay();
 
     for (int step = s.chunks - 1; step >= 0; --step) {
-        const int chunk = chunk_at(s, step), next = step > 0 ? chunk_at(s, step - 1) : chunk;
-        const Rsrc ws = whole(ws_all + size_t(chunk) * Ws::bytes), kw = whole(kw_all + size_t(chunk) * Kw::bytes);
-        Mid ft[kTriBlocks];
-        In fkt[kCt][2], fqt[kCt][2];
+        const int next = step > 0 ? chunk_at(s, step - 1) : chunk_at(s, 0);
+        unsigned char *ahead = lds + (step & 1) * Lds::ahead, *behind = lds + 2 * Lds::ahead + (step & 1) * Lds::behind;
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kTriBlocks; ++i) ft[i] = get<Mid>(ws, Ws::inverse + kTriBlocks * frag_bytes<Mid>, i, lane);
-#pragma unroll
-        for (int ct = 0; ct < kCt; ++ct)
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                fkt[ct][ks] = get<In>(kw, 0, 2 * ct + ks, lane);
-                fqt[ct][ks] = get<In>(kw, Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
-            }
-        requests_stay();
-        const Rsrc to = slab_resource(a.adjoints + (size_t(slab) * s.chunks + chunk) * state_size, unsigned(state_size * 4));
-#pragma unroll
-        for (int ct = 0; ct < kCt; ++ct)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) store4(to, state_offset(s, ct, i, g, col), D[ct][i]);
-        Mid fd[kKs];
-#pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) fd[ks] = from<Mid>(D[2 * ks], D[2 * ks + 1]);
+        for (int ct = 0; ct < kCt; ++ct) tile_put<DK>(behind, ct, r, g, D[ct]);
         share_scalars(scal, raw, lane);
         requests_stay();
         raw = request_scalars(whole(ws_all + size_t(next) * Ws::bytes), lane);
         requests_stay();
-        In fo[2];
-        Mid fod[2];
+        Mid fd[kKs];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            T x[8];
-            float y[8];
-            const f32x4 c[2] = {scalars(scal, kC0, 2 * p, g), scalars(scal, kC0, 2 * p + 1, g)};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = dout[8 * p + j], y[j] = value(x[j]) * c[j >> 2][j & 3];
-            gather(fo[p], x);
-            make(fod[p], y);
-        }
-        requests_stay();
-        load_d_out(next);
-        requests_stay();
+        for (int ks = 0; ks < kKs; ++ks) fd[ks] = from<Mid>(D[2 * ks], D[2 * ks + 1]);
         f32x4 u[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) u[m] = zero;
@@ -161,16 +135,12 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
         load_keys(next);
         requests_stay();
 #pragma unroll
-        for (int m = 0; m < 4; ++m) u[m] *= scalars(scal, kD0, m, g);
+        for (int m = 0; m < 4; ++m) {
+            const f32x4 d = scalars(scal, kD0, m, g), pd = *reinterpret_cast<const f32x4 *>(ahead + 1024 * m + 16 * lane);
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int m = 0; m <= 2 * ks + 1; ++m) mma(u[m], fp[upper_block(m, ks)], fo[ks]);
-        requests_stay();
-        load_scores(next);
-        requests_stay();
-#pragma unroll
-        for (int m = 0; m < 4; ++m) u[m] *= scalars(scal, kBeta, m, g);
+            for (int i = 0; i < 4; ++i) u[m][i] = fmaf(d[i], u[m][i], pd[i]);
+            u[m] *= scalars(scal, kBeta, m, g);
+        }
         const Mid fu[2] = {from<Mid>(u[0], u[1]), from<Mid>(u[2], u[3])};
 #pragma unroll
         for (int m = 0; m < 4; ++m) u[m] = zero;
@@ -178,34 +148,33 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int m = 0; m <= 2 * ks + 1; ++m) mma(u[m], ft[upper_block(m, ks)], fu[ks]);
-        const Rsrc dvr = chunk_rows(a.dv, s, b, h, s.H, s.dv, chunk), rt = float_rows(a.r, s, slab, s.dv, chunk);
-        // accumulator (m, i) is token 32 (m / 2) + 8g + 4 (m % 2) + i, value 4m + i
+        requests_stay();
+        load_inverse(next);
+        requests_stay();
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const f32x4 c = scalars(scal, kC0, m, g), beta = scalars(scal, kBeta, m, g), inverse = scalars(scal, kInverseBeta, m, g);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float w = u[m][i];
-                store_element<T>(dvr, value_at[4 * m + i], fabsf(beta[i]) > 1e-20f ? w : 0.f);
-                store4(rt, r_at[4 * m + i], w * inverse[i]);
-                u[m][i] = w * -c[i];
-            }
+            tile_put<kC>(behind + Tile<DK>::bytes, m, r, g, u[m]);
+            u[m] *= -scalars(scal, kC0, m, g);
         }
         const float all = whole_decay(scal);
         const Mid fw[2] = {from<Mid>(u[0], u[1]), from<Mid>(u[2], u[3])};
 #pragma unroll
-        for (int ct = 0; ct < kCt; ++ct) D[ct] *= all;
+        for (int ct = 0; ct < kCt; ++ct) {
+            const f32x4 qd = *reinterpret_cast<const f32x4 *>(ahead + 4096 + 1024 * ct + 16 * lane);
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int ct = 0; ct < kCt; ++ct) mma(D[ct], fqt[ct][ks], fod[ks]);
+            for (int i = 0; i < 4; ++i) D[ct][i] = fmaf(all, D[ct][i], qd[i]);
+        }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) mma(D[ct], fkt[ct][ks], fw[ks]);
+        requests_stay();
+        load_transposed(next);
+        requests_stay();
     }
+    __syncthreads();
     if (a.d_initial) {
-        const Rsrc to = slab_resource(a.d_initial + slab * state_size, unsigned(state_size * 4));
+        const Rsrc to = slab_resource(a.d_initial + at.slab * state_size, unsigned(state_size * 4));
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
@@ -214,15 +183,142 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
 }
 
 template <typename T, int DK, int N>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(1, 1))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
+__device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Columns &at, unsigned char *lds)
 {
-    __shared__ __align__(16) unsigned char scal[kScalarBytes];
+    using In = typename operands<T, N>::In;
+    using Mid = typename operands<T, N>::Mid;
+    using Mid2 = typename operands<T, 2>::Mid;
+    using Ws = ChunkWs<T, N, true>;
+    using Kw = KeyWs<T, DK, true>;
+    using Lds = AdjointLds<DK>;
+    constexpr int kCt = DK / 16;
+    const Shape &s = a.s;
+    const int lane = at.lane, g = at.g, part = at.col >> 4;
+    const unsigned char *ws_all = a.ws + size_t(at.slab) * s.chunks * Ws::bytes;
+    const unsigned char *kw_all = a.key_ws + (size_t(at.b) * s.Hk + at.hk) * s.chunks * Kw::bytes;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    const unsigned value_pitch = pitch_of<T>(s, s.H, s.dv);
+    unsigned value_at[16];  // value j: token 32 (j / 8) + 8g + j % 8
+#pragma unroll
+    for (int j = 0; j < 16; ++j) value_at[j] = unsigned(token_at(s, 32 * (j >> 3) + 8 * g + (j & 7))) * value_pitch + unsigned(at.col) * unsigned(sizeof(T));
+    const size_t state_bytes = emitted_bytes<T>(DK / 16, s.dv), token_bytes = emitted_bytes<T>(4, s.dv);
+
+    In fqt[kCt][2];
+    Mid fp[kTriBlocks];
+    T dout[16];
+    f32x4 c[4];
+    auto request = [&](int chunk) __attribute__((always_inline)) {
+        const Rsrc ws = whole(ws_all + size_t(chunk) * Ws::bytes), kw = whole(kw_all + size_t(chunk) * Kw::bytes),
+                   dor = chunk_rows(a.d_out, s, at.b, at.h, s.H, s.dv, chunk);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) dout[j] = load_element<T>(dor, value_at[j]);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) c[m] = as_floats(load16(ws, 32u * unsigned(g), 128u * unsigned(m >> 1) + 16u * unsigned(m & 1)));
+#pragma unroll
+        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid>(ws, Ws::scores, i, lane);
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) fqt[ct][ks] = get<In>(kw, Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
+    };
+    auto make_ahead = [&](unsigned char *to) __attribute__((always_inline)) {
+        In fo[2];
+        Mid fod[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            T x[8];
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = dout[8 * p + j], y[j] = value(x[j]) * c[2 * p + (j >> 2)][j & 3];
+            gather(fo[p], x);
+            make(fod[p], y);
+        }
+        f32x4 pd[4], qd[kCt];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) pd[m] = zero;
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct) qd[ct] = zero;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+            for (int m = 0; m <= 2 * ks + 1; ++m) mma(pd[m], fp[upper_block(m, ks)], fo[ks]);
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) mma(qd[ct], fqt[ct][ks], fod[ks]);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4 *>(to + 1024 * m + 16 * lane) = pd[m];
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct) *reinterpret_cast<f32x4 *>(to + 4096 + 1024 * ct + 16 * lane) = qd[ct];
+    };
+    request(chunk_at(s, s.chunks - 1));
+    make_ahead(lds + ((s.chunks - 1) & 1) * Lds::ahead);
+    if (s.chunks > 1) request(chunk_at(s, s.chunks - 2));
+    float inverse[2] = {0.f, 0.f};
+    for (int step = s.chunks - 1; step >= -1; --step) {
+        __syncthreads();
+        const float done[2] = {inverse[0], inverse[1]};  // 1 / beta of the rows that this lane takes away
+        if (step >= 0) {
+            const Rsrc ws = whole(ws_all + size_t(chunk_at(s, step)) * Ws::bytes);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) inverse[i] = load4(ws, 4u * unsigned((64 * i + lane) >> 1), kInverseBeta);
+        }
+        if (step > 0) {
+            make_ahead(lds + ((step - 1) & 1) * Lds::ahead);
+            if (step > 1) {
+                requests_stay();
+                request(chunk_at(s, step - 2));
+                requests_stay();
+            }
+        }
+        if (step + 1 < s.chunks) {
+            const int chunk = chunk_at(s, step + 1);
+            const unsigned char *behind = lds + 2 * Lds::ahead + ((step + 1) & 1) * Lds::behind;
+            const size_t unit = size_t(at.slab) * s.chunks + chunk;
+            const Rsrc to = whole(a.adjoints + unit * state_bytes), tr = whole(a.r + unit * token_bytes),
+                       dvr = chunk_rows(a.dv, s, at.b, at.h, s.H, s.dv, chunk);
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < DK / 32; ++i) {
+                const int item = 64 * i + lane;
+                tile_row<DK>(x, behind, item >> 1, item & 1);
+                emit<Mid2>(to, unpaired(item >> 1), part, item & 1, s.dv, x);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int item = 64 * i + lane, t = item >> 1;
+                tile_row<kC>(x, behind + Tile<DK>::bytes, t, item & 1);
+                float y[8];
+                const bool written = fabsf(done[i]) < 0.99e20f;  // beta is not the stand-in for zero
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    y[j] = written ? x[j] : 0.f;
+                    x[j] *= done[i];
+                }
+                store_row(dvr, unsigned(token_at(s, t)) * value_pitch + unsigned(16 * part + 8 * (item & 1)) * unsigned(sizeof(T)), y, T{});
+                emit<Mid2>(tr, natural(t), part, item & 1, s.dv, x);
+            }
+        }
+    }
+}
+
+// Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'
+template <typename T, int DK, int N>
+__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
+{
+    __shared__ __align__(16) unsigned char lds[AdjointLds<DK>::bytes], scal[kScalarBytes];
     Columns at;
     if (!columns_of(a.s, at)) return;
-    if (blockIdx.y == 0)
-        states<T, DK, N, true>(c, at, scal, nullptr);
-    else
-        adjoint_chain<T, DK, N>(a, at, scal);
+    if (blockIdx.y == 0) {
+        if (threadIdx.x < 64)
+            states<T, DK, N, true>(c, at, scal, lds);
+        else
+            emit_states<T, DK>(c, at, lds);
+    } else {
+        if (threadIdx.x < 64)
+            adjoint_chain<T, DK, N>(a, at, scal, lds);
+        else
+            adjoint_sides<T, DK, N>(a, at, lds);
+    }
 }
 
 template <typename T>
@@ -230,7 +326,7 @@ struct GradientArgs {
     Shape s;
     const T *q, *k, *g, *beta, *d_out;
     T *dq, *dk, *dg, *dbeta;
-    const float *states, *adjoints, *wrong, *r;
+    const unsigned char *states, *adjoints, *wrong, *r;  // fragments, see gd::Tile
     const unsigned char *key_ws;
 };
 
@@ -245,6 +341,37 @@ __device__ __forceinline__ f32x4 four_tokens(const Full &, Rsrc keys, size_t fir
 {
     const unsigned lane = unsigned(r + 16 * (2 * (w & 1) + (g >> 1)));
     return as_floats(load16(keys, 16u * lane + 1024u * unsigned(g & 1), unsigned(first) + unsigned(block) * 2048u));
+}
+
+// a fragment at a lane's offset (0, or nowhere for one that is not there)
+template <typename Frag>
+__device__ __forceinline__ Frag get_at(Rsrc ws, unsigned at, int block, int lane)
+{
+    u32x4 w[planes<Frag>];
+#pragma unroll
+    for (int i = 0; i < planes<Frag>; ++i) w[i] = load16(ws, at | (unsigned(block * planes<Frag> + i) * 1024u + 16u * unsigned(lane)));
+    Frag f;
+    __builtin_memcpy(&f, w, sizeof(f));
+    return f;
+}
+// sum of the products of the lanes' values, added to acc
+__device__ __forceinline__ float dot(const Parts<2> &a, const Parts<2> &b, float acc)
+{
+    u32x4 x[2], y[2];
+    __builtin_memcpy(x, &a, sizeof(a));
+    __builtin_memcpy(y, &b, sizeof(b));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        acc = fmaf(bf16_lo_to_f32(x[0][j]) + bf16_lo_to_f32(x[1][j]), bf16_lo_to_f32(y[0][j]) + bf16_lo_to_f32(y[1][j]), acc);
+        acc = fmaf(bf16_hi_to_f32(x[0][j]) + bf16_hi_to_f32(x[1][j]), bf16_hi_to_f32(y[0][j]) + bf16_hi_to_f32(y[1][j]), acc);
+    }
+    return acc;
+}
+__device__ __forceinline__ float dot(const Full &a, const Full &b, float acc)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc = fmaf(a.v[j], b.v[j], acc);
+    return acc;
 }
 
 // One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  The contractions over value columns take kSlice of them
@@ -298,10 +425,12 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
     for (int ct = 0; ct < kCt; ++ct) dq[ct] = dk[ct] = zero;
 
     for (int h = hk * share; h < (hk + 1) * share; ++h) {
-        const size_t slab = size_t(b) * s.H + h, state_size = size_t(s.dk) * s.dv, state_at = (slab * s.chunks + unsigned(chunk)) * state_size;
-        const Rsrc dor = chunk_rows(a.d_out, s, b, h, s.H, s.dv, chunk), er = float_rows(a.wrong, s, slab, s.dv, chunk),
-                   rr = float_rows(a.r, s, slab, s.dv, chunk), Sr = slab_resource(a.states + state_at, unsigned(state_size * 4)),
-                   Dr = slab_resource(a.adjoints + state_at, unsigned(state_size * 4));
+        const size_t slab = size_t(b) * s.H + h, value_unit = slab * s.chunks + unsigned(chunk);
+        const size_t state_bytes = emitted_bytes<T>(kCt, s.dv), token_bytes = emitted_bytes<T>(4, s.dv);
+        const Rsrc dor = chunk_rows(a.d_out, s, b, h, s.H, s.dv, chunk), er = whole(a.wrong + value_unit * token_bytes),
+                   rr = whole(a.r + value_unit * token_bytes), Sr = whole(a.states + value_unit * state_bytes),
+                   Dr = whole(a.adjoints + value_unit * state_bytes);
+        const int blocks = value_blocks(s.dv);
         const unsigned own = unsigned(token_at(s, 16 * w + r));
         if (w == 0) {
             const Rsrc gr = chunk_rows(a.g, s, b, h, s.H, 1, chunk), br = chunk_rows(a.beta, s, b, h, s.H, 1, chunk);
@@ -314,41 +443,28 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
         for (int n = 0; n < 4; ++n) x[n] = y[n] = zero;
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) read[ct] = erase[ct] = write[ct] = zero;
-        float db = 0.f, ds = 0.f;  // dbeta, <D, S>
-        for (int v0 = 0; v0 < s.dv; v0 += kSlice) {
+        float ds = 0.f;  // <D, S>
+        for (int v0 = 0; v0 < blocks; v0 += kVs) {
             In fo[kVs];
             Mid fr[kVs], fe[kVs];
 #pragma unroll
             for (int ks = 0; ks < kVs; ++ks) {
-                const int c = v0 + 32 * ks + 8 * g;
-                const bool has = c < s.dv;
-                load_row(fo[ks], dor, has ? own * pitch_of<T>(s, s.H, s.dv) + unsigned(c) * unsigned(sizeof(T)) : kNowhere);
-                const unsigned at = has ? 4u * (own * unsigned(s.dv) + unsigned(c)) : kNowhere;
-                float e8[8], r8[8];
-                load8(e8, er, at);
-                load8(r8, rr, at);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) db = fmaf(e8[j], r8[j], db);
-                make(fe[ks], e8);
-                make(fr[ks], r8);
+                const bool has = v0 + ks < blocks;
+                load_row(fo[ks], dor, row_offset<T>(pitch_of<T>(s, s.H, s.dv), int(own), v0 + ks, g, s.dv));
+                const unsigned nowhere = has ? 0u : kNowhere;
+                fe[ks] = get_at<Mid>(er, nowhere, w * blocks + v0 + ks, lane);
+                fr[ks] = get_at<Mid>(rr, nowhere, w * blocks + v0 + ks, lane);
                 lds_put(wrong, w * kVs + ks, lane, fe[ks]);
             }
 #pragma unroll
             for (int o = 0; o < (kCt * kVs + 3) / 4; ++o) {
                 const int block = 4 * o + w, ct = block / kVs, ks = block % kVs;
                 if (kCt * kVs % 4 != 0 && block >= kCt * kVs) break;
-                const int channel = paired(ct, r), c = v0 + 32 * ks + 8 * g;
-                const unsigned at = channel < s.dk && c < s.dv ? 4u * (unsigned(channel) * unsigned(s.dv) + unsigned(c)) : kNowhere;
-                float s8[8], d8[8];
-                load8(s8, Sr, at);
-                load8(d8, Dr, at);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) ds = fmaf(s8[j], d8[j], ds);
-                Mid f;
-                make(f, s8);
-                lds_put(fS, block, lane, f);
-                make(f, d8);
-                lds_put(fD, block, lane, f);
+                const unsigned nowhere = v0 + ks < blocks ? 0u : kNowhere;
+                const Mid fs = get_at<Mid>(Sr, nowhere, ct * blocks + v0 + ks, lane), fd = get_at<Mid>(Dr, nowhere, ct * blocks + v0 + ks, lane);
+                ds = dot(fs, fd, ds);
+                lds_put(fS, block, lane, fs);
+                lds_put(fD, block, lane, fd);
             }
             __syncthreads();
 #pragma unroll
@@ -370,13 +486,11 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
             }
             __syncthreads();
         }
-        db += __shfl_xor(db, 16);
-        db += __shfl_xor(db, 32);
-        if (g == 0) store_element<T>(chunk_rows(a.dbeta, s, b, h, s.H, 1, chunk), own * pitch_of<T>(s, s.H, 1), db);
         ds = wave_total(ds);
         if (lane == 0) through[w] = ds;
 
         // X, Y and the pairs' part of dg
+        const Rsrc dbr = chunk_rows(a.dbeta, s, b, h, s.H, 1, chunk);
         float carry[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
@@ -386,6 +500,8 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
             for (int i = 0; i < 4; ++i) {
                 const int t = 16 * w + 4 * g + i;
                 float xi = 0.f, yi = 0.f;
+                if (n == w && r == 4 * g + i)  // r_t . e_t
+                    store_element<T>(dbr, unsigned(token_at(s, t)) * pitch_of<T>(s, s.H, 1), y[n][i]);
                 if (n <= w) {
                     const float decay = c <= t ? expf(float(sum[t] - sum[c])) * bet[c] : 0.f;
                     xi = decay * x[n][i];
@@ -467,16 +583,25 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
         }
         __syncthreads();
     }
+    // rows of dq and dk through the wave's own part of LDS: 16 bytes a lane
+    constexpr int kRowPitch = DK + 8;
+    T *rows = reinterpret_cast<T *>(shared) + 16 * w * kRowPitch;
     const Rsrc dqr = chunk_rows(a.dq, s, b, hk, s.Hk, s.dk, chunk), dkr = chunk_rows(a.dk, s, b, hk, s.Hk, s.dk, chunk);
 #pragma unroll
-    for (int ct = 0; ct < kCt; ++ct) {
-        const int c = paired(ct, r);
+    for (int which = 0; which < 2; ++which) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned at = c < s.dk ? unsigned(token_at(s, 16 * w + 4 * g + i)) * key_pitch + unsigned(c) * unsigned(sizeof(T)) : kNowhere;
-            store_element<T>(dqr, at, dq[ct][i]);
-            store_element<T>(dkr, at, dk[ct][i]);
+        for (int ct = 0; ct < kCt; ++ct)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) io<T>::store(rows + (4 * g + i) * kRowPitch + paired(ct, r), which == 0 ? dq[ct][i] : dk[ct][i]);
+        wave_fence();
+        constexpr int kPiece = 16 / int(sizeof(T)), kPieces = DK / kPiece;
+#pragma unroll
+        for (int o = 0; o < 16 * kPieces / 64; ++o) {
+            const int item = 64 * o + lane, t = item / kPieces, c = (item % kPieces) * kPiece;
+            const unsigned to = c < s.dk ? unsigned(token_at(s, 16 * w + t)) * key_pitch + unsigned(c) * unsigned(sizeof(T)) : kNowhere;
+            __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const u32x4 *>(rows + t * kRowPitch + c), which == 0 ? dqr : dkr, to, 0, 0);
         }
+        wave_fence();
     }
 }
 
@@ -490,10 +615,10 @@ Buffers buffers(const Shape &s)
     Buffers at;
     at.key_ws = round256(units * ChunkWs<T, N, true>::bytes);
     at.states = at.key_ws + round256(size_t(s.B) * s.Hk * s.chunks * KeyWs<T, DK, true>::bytes);
-    at.adjoints = at.states + round256(units * s.dk * s.dv * 4);
-    at.wrong = at.adjoints + round256(units * s.dk * s.dv * 4);
-    at.r = at.wrong + round256(slabs * s.L * s.dv * 4);
-    at.bytes = at.r + round256(slabs * s.L * s.dv * 4);
+    at.adjoints = at.states + units * emitted_bytes<T>(DK / 16, s.dv);
+    at.wrong = at.adjoints + units * emitted_bytes<T>(DK / 16, s.dv);
+    at.r = at.wrong + units * emitted_bytes<T>(4, s.dv);
+    at.bytes = at.r + units * emitted_bytes<T>(4, s.dv);
     return at;
 }
 
@@ -505,8 +630,7 @@ hipError_t launch(const Shape &s, const GradientPointers &p, void *workspace, hi
     const Buffers at = buffers<T, DK, N>(s);
     const T *q = static_cast<const T *>(p.q), *k = static_cast<const T *>(p.k), *v = static_cast<const T *>(p.v), *g = static_cast<const T *>(p.g),
             *beta = static_cast<const T *>(p.beta), *d_out = static_cast<const T *>(p.d_out);
-    float *S = reinterpret_cast<float *>(ws + at.states), *D = reinterpret_cast<float *>(ws + at.adjoints), *e = reinterpret_cast<float *>(ws + at.wrong),
-          *r = reinterpret_cast<float *>(ws + at.r);
+    unsigned char *S = ws + at.states, *D = ws + at.adjoints, *e = ws + at.wrong, *r = ws + at.r;
     const PrepareArgs<T> prepare = {s, q, k, g, beta, ws, ws + at.key_ws};
     const ChainArgs<T> chain = {s, q, k, v, p.initial, nullptr, nullptr, S, e, ws, ws + at.key_ws};
     const AdjointArgs<T> adjoint = {s, k, d_out, p.d_final, static_cast<T *>(p.dv), p.d_initial, D, r, ws, ws + at.key_ws};
@@ -514,7 +638,7 @@ hipError_t launch(const Shape &s, const GradientPointers &p, void *workspace, hi
                                       static_cast<T *>(p.dbeta), S, D, e, r, ws + at.key_ws};
     const LaunchTimer timer(kKernelGatedDeltaBackward, stream);
     gd_prepare<T, DK, N, true><<<slabs * unsigned(s.chunks), 256, 0, stream>>>(prepare);
-    gd_both_chains<T, DK, N><<<dim3((slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 2), 64, 0, stream>>>(chain, adjoint);
+    gd_both_chains<T, DK, N><<<dim3((slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 2), 128, 0, stream>>>(chain, adjoint);
     const unsigned key_units = unsigned(s.B) * unsigned(s.Hk) * unsigned(s.chunks);
     gd_gradients<T, DK><<<key_units, 256, 0, stream>>>(gradient);
     return hipGetLastError();

@@ -17,7 +17,7 @@ struct ChainArgs {
     const float *initial;                 // [B, H, dk, dv] or null
     T *out;                               // forward
     float *final_state;                   // [B, H, dk, dv] or null
-    float *states, *wrong;                // gradient: S of every chunk [slab][chunk][dk][dv], e [slab][L][dv]
+    unsigned char *states, *wrong;        // gradient: S and e of every chunk as fragments, see Emitted
     const unsigned char *ws, *key_ws;
 };
 
@@ -51,9 +51,7 @@ __device__ __forceinline__ u32x4 request_scalars(Rsrc ws, int lane) { return loa
 __device__ __forceinline__ void share_scalars(unsigned char *lds, const u32x4 &x, int lane)
 {
     *reinterpret_cast<u32x4 *>(lds + 16 * lane) = x;
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    wave_fence();
 }
 // of the tokens that accumulators of tile m stand for
 enum Scalar { kC0 = 0, kBeta = 256, kD0 = 512, kInverseBeta = 768 };
@@ -115,9 +113,59 @@ __device__ __forceinline__ bool columns_of(const Shape &s, Columns &c)
     return true;
 }
 
+// What the chains of the gradient leave: a state (DK rows) or 64 tokens' rows, 16 columns a wave, first in LDS as [column][row] tiles of floats, which a
+// second wave takes to the workspace as fragments of two parts: rows by 16 in tiles, columns along the products.
+template <int kRows>
+struct Tile {
+    static constexpr int pitch = kRows + 4, bytes = 16 * pitch * 4;
+};
+template <int kRows>
+__device__ __forceinline__ void tile_put(unsigned char *lds, int tile, int r, int g, const f32x4 &x)  // rows paired(tile, 4g) .. + 3 of column r
+{
+    *reinterpret_cast<f32x4 *>(lds + 4 * (r * Tile<kRows>::pitch + paired(tile, 4 * g))) = x;
+}
+inline __host__ __device__ int value_blocks(int dv) { return (dv + 31) / 32; }
+template <typename T>
+constexpr size_t row_block_bytes = frag_bytes<typename operands<T, 2>::Mid>;
+// bytes of `tiles` tiles of 16 rows
+template <typename T>
+__host__ __device__ __forceinline__ size_t emitted_bytes(int tiles, int dv)
+{
+    return size_t(tiles) * value_blocks(dv) * row_block_bytes<T>;
+}
+// row -> its tile and its place in it
+struct Place {
+    int tile, r;
+};
+__device__ __forceinline__ Place natural(int row) { return {row >> 4, row & 15}; }
+__device__ __forceinline__ Place unpaired(int row) { return {2 * (row >> 5) + ((row >> 2) & 1), 4 * ((row >> 3) & 3) + (row & 3)}; }
+
+// eight columns of a row as a fragment's lane; where the head has 16 columns only, the other half of the fragment is zero
+template <typename Mid2>
+__device__ __forceinline__ void emit(Rsrc to, Place at, int part, int group, int dv, const float (&x)[8])
+{
+    Mid2 f;
+    make(f, x);
+    u32x4 w[planes<Mid2>];
+    __builtin_memcpy(w, &f, sizeof(f));
+    const unsigned block = unsigned(at.tile * value_blocks(dv) + (part >> 1)) * unsigned(frag_bytes<Mid2>);
+    const unsigned off = block + 16u * unsigned(at.r + 16 * (2 * (part & 1) + group));
+#pragma unroll
+    for (int p = 0; p < planes<Mid2>; ++p) {
+        __builtin_amdgcn_raw_buffer_store_b128(w[p], to, off + 1024u * unsigned(p), 0, 0);
+        if (dv == 16) __builtin_amdgcn_raw_buffer_store_b128(u32x4{0, 0, 0, 0}, to, off + 512u + 1024u * unsigned(p), 0, 0);
+    }
+}
+template <int kRows>
+__device__ __forceinline__ void tile_row(float (&x)[8], const unsigned char *lds, int row, int group)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const float *>(lds + 4 * ((8 * group + j) * Tile<kRows>::pitch + row));
+}
+
 template <typename T, int DK, int N, bool kBwd>
 __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at, unsigned char *scal /* the wave's scalars */,
-                                       unsigned char *lds /* two HandOvers; forward */)
+                                       unsigned char *lds /* two HandOvers, or two state and two token tiles */)
 {
     using In = typename operands<T, N>::In;
     using Mid = typename operands<T, N>::Mid;
@@ -135,14 +183,13 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
 
     // offsets of a lane's rows: of keys, and of its 16 values
     const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk), value_pitch = pitch_of<T>(s, s.H, s.dv);
-    unsigned key_at[4], value_at[16], e_at[16];
+    unsigned key_at[4], value_at[16];
 #pragma unroll
     for (int m = 0; m < 4; ++m) key_at[m] = row_offset<T>(key_pitch, token_at(s, paired(m, r)), 0, g, s.dk);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
         const unsigned t = unsigned(token_at(s, paired(j >> 2, 4 * g + (j & 3))));
         value_at[j] = t * value_pitch + unsigned(col) * unsigned(sizeof(T));
-        e_at[j] = 4u * (t * unsigned(s.dv) + unsigned(col));
     }
 
     f32x4 S[kCt];
@@ -198,13 +245,11 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
 
     for (int step = 0; step < s.chunks; ++step) {
         const int chunk = chunk_at(s, step), next = step + 1 < s.chunks ? chunk_at(s, step + 1) : chunk;
-        unsigned char *hand = lds + (step & 1) * Hand::bytes;
+        unsigned char *hand = lds + (step & 1) * (kBwd ? Tile<DK>::bytes + Tile<kC>::bytes : Hand::bytes);
         if constexpr (kBwd) {
-            const Rsrc to = slab_resource(a.states + (size_t(slab) * s.chunks + chunk) * state_size, unsigned(state_size * 4));
+            __syncthreads();
 #pragma unroll
-            for (int ct = 0; ct < kCt; ++ct)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) store4(to, state_offset(s, ct, i, g, col), S[ct][i]);
+            for (int ct = 0; ct < kCt; ++ct) tile_put<DK>(hand, ct, r, g, S[ct]);
         }
         share_scalars(scal, raw, lane);
         requests_stay();
@@ -246,9 +291,8 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
         load_inverse(next);
         requests_stay();
         if constexpr (kBwd) {
-            const Rsrc to = float_rows(a.wrong, s, slab, s.dv, chunk);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) store4(to, e_at[j], e[j >> 2][j & 3]);
+            for (int m = 0; m < 4; ++m) tile_put<kC>(hand + Tile<DK>::bytes, m, r, g, e[m]);
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
@@ -269,12 +313,43 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
         requests_stay();
         if constexpr (!kBwd) __syncthreads();
     }
-    if (a.final_state) {
+    if constexpr (kBwd) __syncthreads();
+    if (!kBwd && a.final_state) {
         const Rsrc to = slab_resource(a.final_state + slab * state_size, unsigned(state_size * 4));
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
             for (int i = 0; i < 4; ++i) store4(to, state_offset(s, ct, i, g, col), S[ct][i]);
+    }
+}
+
+// S and e of the gradient's chain to the workspace, one chunk behind it
+template <typename T, int DK>
+__device__ __forceinline__ void emit_states(const ChainArgs<T> &a, const Columns &at, const unsigned char *lds)
+{
+    using Mid2 = typename operands<T, 2>::Mid;
+    const Shape &s = a.s;
+    const int part = at.col >> 4;
+    const size_t state_bytes = emitted_bytes<T>(DK / 16, s.dv), token_bytes = emitted_bytes<T>(4, s.dv);
+    for (int step = 0; step <= s.chunks; ++step) {
+        __syncthreads();
+        if (step == 0) continue;
+        const unsigned char *hand = lds + ((step - 1) & 1) * (Tile<DK>::bytes + Tile<kC>::bytes);
+        const size_t unit = size_t(at.slab) * s.chunks + chunk_at(s, step - 1);
+        const Rsrc to = whole(a.states + unit * state_bytes), te = whole(a.wrong + unit * token_bytes);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < DK / 32; ++i) {
+            const int item = 64 * i + at.lane;
+            tile_row<DK>(x, hand, item >> 1, item & 1);
+            emit<Mid2>(to, unpaired(item >> 1), part, item & 1, s.dv, x);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int item = 64 * i + at.lane;
+            tile_row<kC>(x, hand + Tile<DK>::bytes, item >> 1, item & 1);
+            emit<Mid2>(te, natural(item >> 1), part, item & 1, s.dv, x);
+        }
     }
 }
 
