@@ -270,6 +270,38 @@ __device__ __forceinline__ Rsrc chunk_rows(const T *all, const Shape &s, int b, 
     const unsigned rows = unsigned(s.L - chunk * kC < kC ? s.L - chunk * kC : kC);
     return slab_resource(all + first * width, (rows - 1) * pitch_of<T>(s, heads, width) + unsigned(width) * unsigned(sizeof(T)));
 }
+// What a chain of chunks reads or writes in turn: a pointer that moves by a constant, so that a step forms a resource with a few scalar
+// instructions.  Chunks are full but for the sequence's last one.
+struct Walk {
+    const unsigned char *p;
+    long step;
+    unsigned extent, last_extent;
+    int chunk, move, last_chunk;
+
+    __device__ __forceinline__ Rsrc here() const { return slab_resource(p, chunk == last_chunk ? last_extent : extent); }
+    __device__ __forceinline__ void next() { p += step, chunk += move; }
+};
+// `first`: the chunk it starts with, `move`: +1 or -1
+template <typename T>
+__device__ __forceinline__ Walk walk_rows(const T *all, const Shape &s, int b, int head, int heads, int width, int first, int move)
+{
+    const unsigned pitch = pitch_of<T>(s, heads, width), row = unsigned(width) * unsigned(sizeof(T));
+    const size_t L = size_t(s.L), at = s.token_major ? size_t(b) * L * heads + head : (size_t(b) * heads + head) * L;
+    Walk w;
+    w.p = reinterpret_cast<const unsigned char *>(all + at * width) + long(first) * kC * long(pitch);
+    w.step = long(move) * kC * long(pitch);
+    w.extent = (kC - 1) * pitch + row;
+    w.last_extent = unsigned(s.L - (s.chunks - 1) * kC - 1) * pitch + row;
+    w.chunk = first;
+    w.move = move;
+    w.last_chunk = s.chunks - 1;
+    return w;
+}
+// blocks of `bytes` each, one a chunk
+__device__ __forceinline__ Walk walk_blocks(const unsigned char *all, size_t bytes, int first, int move)
+{
+    return {all + long(first) * long(bytes), long(move) * long(bytes), 0x80000000u, 0x80000000u, first, move, first};
+}
 // everything from p on
 __device__ __forceinline__ Rsrc whole(const void *p) { return slab_resource(p, 0x80000000u); }
 // where a lane's part of a fragment's row is: channels 32 step + 8g .. + 7 of a token; channels that the head does not have are nowhere

@@ -79,47 +79,49 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
             for (int i = 0; i < 4; ++i) D[ct][i] = load4(from0, state_offset(s, ct, i, g, col));
     }
 
+    const int first = chunk_at(s, s.chunks - 1), move = s.reverse ? 1 : -1;
+    Walk kr = walk_rows(a.k, s, at.b, at.hk, s.Hk, s.dk, first, move), ws = walk_blocks(ws_all, Ws::bytes, first, move),
+         kw = walk_blocks(kw_all, Kw::bytes, first, move);
     In fk[4][kKs], fkt[kCt][2];
     Mid ft[kTriBlocks];
-    auto load_keys = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc kr = chunk_rows(a.k, s, at.b, at.hk, s.Hk, s.dk, chunk);
+    auto load_keys = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = kr.here();
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
-            for (int m = 0; m < 4; ++m) load_row(fk[m][ks], kr, key_at[m] + 32u * unsigned(ks * sizeof(T)));
+            for (int m = 0; m < 4; ++m) load_row(fk[m][ks], from0, key_at[m] + 32u * unsigned(ks * sizeof(T)));
     };
-    auto load_inverse = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc ws = whole(ws_all + size_t(chunk) * Ws::bytes);
+    auto load_inverse = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = ws.here();
 #pragma unroll
-        for (int i = 0; i < kTriBlocks; ++i) ft[i] = get<Mid>(ws, Ws::inverse + kTriBlocks * frag_bytes<Mid>, i, lane);
+        for (int i = 0; i < kTriBlocks; ++i) ft[i] = get<Mid>(from0, Ws::inverse + kTriBlocks * frag_bytes<Mid>, i, lane);
     };
-    auto load_transposed = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc kw = whole(kw_all + size_t(chunk) * Kw::bytes);
+    auto load_transposed = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = kw.here();
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int ct = 0; ct < kCt; ++ct) fkt[ct][ks] = get<In>(kw, 0, 2 * ct + ks, lane);
+            for (int ct = 0; ct < kCt; ++ct) fkt[ct][ks] = get<In>(from0, 0, 2 * ct + ks, lane);
     };
     // (in the order of the loop, see gd::states)
-    const int first = chunk_at(s, s.chunks - 1);
-    u32x4 raw = request_scalars(whole(ws_all + size_t(first) * Ws::bytes), lane);
+    u32x4 raw = request_scalars(ws.here(), lane);
     requests_stay();
-    load_keys(first);
+    load_keys();
     requests_stay();
-    load_inverse(first);
+    load_inverse();
     requests_stay();
-    load_transposed(first);
+    load_transposed();
     requests_stay();
 
     for (int step = s.chunks - 1; step >= 0; --step) {
-        const int next = step > 0 ? chunk_at(s, step - 1) : chunk_at(s, 0);
+        if (step > 0) kr.next(), ws.next(), kw.next();  // what is requested from here on
         unsigned char *ahead = lds + (step & 1) * Lds::ahead, *behind = lds + 2 * Lds::ahead + (step & 1) * Lds::behind;
         __syncthreads();
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) tile_put<DK>(behind, ct, r, g, D[ct]);
         share_scalars(scal, raw, lane);
         requests_stay();
-        raw = request_scalars(whole(ws_all + size_t(next) * Ws::bytes), lane);
+        raw = request_scalars(ws.here(), lane);
         requests_stay();
         Mid fd[kKs];
 #pragma unroll
@@ -132,7 +134,7 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
 #pragma unroll
             for (int m = 0; m < 4; ++m) mma(u[m], fk[m][ks], fd[ks]);
         requests_stay();
-        load_keys(next);
+        load_keys();
         requests_stay();
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
@@ -149,7 +151,7 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
 #pragma unroll
             for (int m = 0; m <= 2 * ks + 1; ++m) mma(u[m], ft[upper_block(m, ks)], fu[ks]);
         requests_stay();
-        load_inverse(next);
+        load_inverse();
         requests_stay();
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
@@ -169,7 +171,7 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) mma(D[ct], fkt[ct][ks], fw[ks]);
         requests_stay();
-        load_transposed(next);
+        load_transposed();
         requests_stay();
     }
     __syncthreads();
@@ -183,7 +185,8 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
 }
 
 template <typename T, int DK, int N>
-__device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Columns &at, unsigned char *lds)
+__device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Columns &at, unsigned char *own /* the wave's: scalars, then a strip */,
+                                              unsigned char *lds)
 {
     using In = typename operands<T, N>::In;
     using Mid = typename operands<T, N>::Mid;
@@ -194,42 +197,48 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
     constexpr int kCt = DK / 16;
     const Shape &s = a.s;
     const int lane = at.lane, g = at.g, part = at.col >> 4;
-    const unsigned char *ws_all = a.ws + size_t(at.slab) * s.chunks * Ws::bytes;
-    const unsigned char *kw_all = a.key_ws + (size_t(at.b) * s.Hk + at.hk) * s.chunks * Kw::bytes;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     const unsigned value_pitch = pitch_of<T>(s, s.H, s.dv);
-    unsigned value_at[16];  // value j: token 32 (j / 8) + 8g + j % 8
+    unsigned value_at[Strip<T>::loads];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) value_at[j] = unsigned(token_at(s, 32 * (j >> 3) + 8 * g + (j & 7))) * value_pitch + unsigned(at.col) * unsigned(sizeof(T));
-    const size_t state_bytes = emitted_bytes<T>(DK / 16, s.dv), token_bytes = emitted_bytes<T>(4, s.dv);
+    for (int l = 0; l < Strip<T>::loads; ++l) value_at[l] = strip_offset<T>(s, value_pitch, part, lane, l);
+    const size_t state_bytes = emitted_bytes<T>(DK / 16, s.dv), token_bytes = emitted_bytes<T>(4, s.dv), units = size_t(at.slab) * s.chunks;
 
+    const int first = chunk_at(s, s.chunks - 1), move = s.reverse ? 1 : -1;
+    Walk dor = walk_rows(a.d_out, s, at.b, at.h, s.H, s.dv, first, move), dvr = walk_rows(static_cast<const T *>(a.dv), s, at.b, at.h, s.H, s.dv, first, move),
+         ws = walk_blocks(a.ws + units * Ws::bytes, Ws::bytes, first, move), inv = ws,
+         kw = walk_blocks(a.key_ws + (size_t(at.b) * s.Hk + at.hk) * s.chunks * Kw::bytes, Kw::bytes, first, move),
+         to_d = walk_blocks(a.adjoints + units * state_bytes, state_bytes, first, move), to_r = walk_blocks(a.r + units * token_bytes, token_bytes, first, move);
     In fqt[kCt][2];
     Mid fp[kTriBlocks];
-    T dout[16];
-    f32x4 c[4];
-    auto request = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc ws = whole(ws_all + size_t(chunk) * Ws::bytes), kw = whole(kw_all + size_t(chunk) * Kw::bytes),
-                   dor = chunk_rows(a.d_out, s, at.b, at.h, s.H, s.dv, chunk);
+    Strip<T> dout;
+    u32x4 raw;
+    auto request = [&]() __attribute__((always_inline)) {
+        const Rsrc ws0 = ws.here(), kw0 = kw.here(), do0 = dor.here();
+        ws.next(), kw.next(), dor.next();
+        raw = request_scalars(ws0, lane);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) dout[j] = load_element<T>(dor, value_at[j]);
+        for (int l = 0; l < Strip<T>::loads; ++l) dout.w[l] = load16(do0, value_at[l]);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) c[m] = as_floats(load16(ws, 32u * unsigned(g), 128u * unsigned(m >> 1) + 16u * unsigned(m & 1)));
-#pragma unroll
-        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid>(ws, Ws::scores, i, lane);
+        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid>(ws0, Ws::scores, i, lane);
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) fqt[ct][ks] = get<In>(kw, Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
+            for (int ks = 0; ks < 2; ++ks) fqt[ct][ks] = get<In>(kw0, Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
     };
     auto make_ahead = [&](unsigned char *to) __attribute__((always_inline)) {
         In fo[2];
         Mid fod[2];
+        strip_put(own + kScalarBytes, dout, lane);
+        share_scalars(own, raw, lane);
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
             T x[8];
             float y[8];
+            strip_column(x, own + kScalarBytes, p, at.r, g);
+            const f32x4 c[2] = {scalars(own, kC0, 2 * p, g), scalars(own, kC0, 2 * p + 1, g)};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = dout[8 * p + j], y[j] = value(x[j]) * c[2 * p + (j >> 2)][j & 3];
+            for (int j = 0; j < 8; ++j) y[j] = value(x[j]) * c[j >> 2][j & 3];
             gather(fo[p], x);
             make(fod[p], y);
         }
@@ -250,32 +259,31 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) *reinterpret_cast<f32x4 *>(to + 4096 + 1024 * ct + 16 * lane) = qd[ct];
     };
-    request(chunk_at(s, s.chunks - 1));
+    request();
     make_ahead(lds + ((s.chunks - 1) & 1) * Lds::ahead);
-    if (s.chunks > 1) request(chunk_at(s, s.chunks - 2));
+    if (s.chunks > 1) request();
     float inverse[2] = {0.f, 0.f};
     for (int step = s.chunks - 1; step >= -1; --step) {
         __syncthreads();
         const float done[2] = {inverse[0], inverse[1]};  // 1 / beta of the rows that this lane takes away
         if (step >= 0) {
-            const Rsrc ws = whole(ws_all + size_t(chunk_at(s, step)) * Ws::bytes);
+            const Rsrc ws0 = inv.here();
+            inv.next();
 #pragma unroll
-            for (int i = 0; i < 2; ++i) inverse[i] = load4(ws, 4u * unsigned((64 * i + lane) >> 1), kInverseBeta);
+            for (int i = 0; i < 2; ++i) inverse[i] = load4(ws0, 4u * unsigned((64 * i + lane) >> 1), kInverseBeta);
         }
         if (step > 0) {
             make_ahead(lds + ((step - 1) & 1) * Lds::ahead);
             if (step > 1) {
                 requests_stay();
-                request(chunk_at(s, step - 2));
+                request();
                 requests_stay();
             }
         }
         if (step + 1 < s.chunks) {
-            const int chunk = chunk_at(s, step + 1);
             const unsigned char *behind = lds + 2 * Lds::ahead + ((step + 1) & 1) * Lds::behind;
-            const size_t unit = size_t(at.slab) * s.chunks + chunk;
-            const Rsrc to = whole(a.adjoints + unit * state_bytes), tr = whole(a.r + unit * token_bytes),
-                       dvr = chunk_rows(a.dv, s, at.b, at.h, s.H, s.dv, chunk);
+            const Rsrc to = to_d.here(), tr = to_r.here(), dv0 = dvr.here();
+            to_d.next(), to_r.next(), dvr.next();
             float x[8];
 #pragma unroll
             for (int i = 0; i < DK / 32; ++i) {
@@ -294,7 +302,7 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
                     y[j] = written ? x[j] : 0.f;
                     x[j] *= done[i];
                 }
-                store_row(dvr, unsigned(token_at(s, t)) * value_pitch + unsigned(16 * part + 8 * (item & 1)) * unsigned(sizeof(T)), y, T{});
+                store_row(dv0, unsigned(token_at(s, t)) * value_pitch + unsigned(16 * part + 8 * (item & 1)) * unsigned(sizeof(T)), y, T{});
                 emit<Mid2>(tr, natural(t), part, item & 1, s.dv, x);
             }
         }
@@ -303,9 +311,9 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
 
 // Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'
 template <typename T, int DK, int N>
-__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
+__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(DK <= 64 ? 2 : 1, DK <= 64 ? 2 : 1))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
 {
-    __shared__ __align__(16) unsigned char lds[AdjointLds<DK>::bytes], scal[kScalarBytes];
+    __shared__ __align__(16) unsigned char lds[AdjointLds<DK>::bytes], scal[kScalarBytes + Strip<T>::bytes], own[kScalarBytes + Strip<T>::bytes];
     Columns at;
     if (!columns_of(a.s, at)) return;
     if (blockIdx.y == 0) {
@@ -317,7 +325,7 @@ __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         if (threadIdx.x < 64)
             adjoint_chain<T, DK, N>(a, at, scal, lds);
         else
-            adjoint_sides<T, DK, N>(a, at, lds);
+            adjoint_sides<T, DK, N>(a, at, own, lds);
     }
 }
 

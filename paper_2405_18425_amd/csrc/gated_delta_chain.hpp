@@ -113,6 +113,48 @@ __device__ __forceinline__ bool columns_of(const Shape &s, Columns &c)
     return true;
 }
 
+// The 16 columns of a chunk's 64 rows of values: requested as rows, 16 bytes a lane, and read back from LDS by column, tokens 32p + 8g .. + 7 of
+// column r.  (One element a lane would be 16 requests instead of 2, each as long in the address unit as one of 16 bytes.)
+template <typename T>
+struct Strip {
+    static constexpr int pieces = 16 * int(sizeof(T)) / 16, loads = pieces;  // 16-byte pieces of a row; a load takes 64 / pieces rows
+    static constexpr int pitch = sizeof(T) == 2 ? 16 : 17, bytes = kC * pitch * int(sizeof(T));
+    u32x4 w[loads];
+};
+template <typename T>
+__device__ __forceinline__ unsigned strip_offset(const Shape &s, unsigned pitch, int part, int lane, int load)
+{
+    constexpr int kPieces = Strip<T>::pieces;
+    const int t = load * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
+    return unsigned(token_at(s, t)) * pitch + unsigned(16 * part) * unsigned(sizeof(T)) + 16u * unsigned(piece);
+}
+template <typename T>
+__device__ __forceinline__ void strip_put(unsigned char *lds, const Strip<T> &x, int lane)
+{
+    constexpr int kPieces = Strip<T>::pieces;
+#pragma unroll
+    for (int l = 0; l < Strip<T>::loads; ++l) {
+        const int t = l * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<u32x4 *>(lds + t * 32 + 16 * piece) = x.w[l];
+        else  // rows of 17 floats: columns are read without bank conflicts
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<unsigned *>(lds + 4 * (t * 17 + 4 * piece + i)) = x.w[l][i];
+    }
+}
+// tokens 32 p + 8g .. + 7 of column r
+__device__ __forceinline__ void strip_column(bf16_t (&x)[8], const unsigned char *lds, int p, int r, int g)
+{
+    const uint16_t *q = reinterpret_cast<const uint16_t *>(lds) + (32 * p + 8 * g + (r >> 2)) * 16 + 4 * (r & 3);
+    const bf16x8 v = join(lds_read_tr(q), lds_read_tr(q + 4 * 16));
+    __builtin_memcpy(x, &v, sizeof(v));
+}
+__device__ __forceinline__ void strip_column(float (&x)[8], const unsigned char *lds, int p, int r, int g)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const float *>(lds + 4 * ((32 * p + 8 * g + j) * 17 + r));
+}
+
 // What the chains of the gradient leave: a state (DK rows) or 64 tokens' rows, 16 columns a wave, first in LDS as [column][row] tiles of floats, which a
 // second wave takes to the workspace as fragments of two parts: rows by 16 in tiles, columns along the products.
 template <int kRows>
@@ -164,7 +206,7 @@ __device__ __forceinline__ void tile_row(float (&x)[8], const unsigned char *lds
 }
 
 template <typename T, int DK, int N, bool kBwd>
-__device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at, unsigned char *scal /* the wave's scalars */,
+__device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at, unsigned char *scal /* the wave's: scalars, then a strip */,
                                        unsigned char *lds /* two HandOvers, or two state and two token tiles */)
 {
     using In = typename operands<T, N>::In;
@@ -181,16 +223,13 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
     const size_t state_size = size_t(s.dk) * s.dv;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
-    // offsets of a lane's rows: of keys, and of its 16 values
-    const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk), value_pitch = pitch_of<T>(s, s.H, s.dv);
-    unsigned key_at[4], value_at[16];
+    // offsets of a lane's rows of keys, and of its pieces of values
+    const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk);
+    unsigned key_at[4], value_at[Strip<T>::loads];
 #pragma unroll
     for (int m = 0; m < 4; ++m) key_at[m] = row_offset<T>(key_pitch, token_at(s, paired(m, r)), 0, g, s.dk);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const unsigned t = unsigned(token_at(s, paired(j >> 2, 4 * g + (j & 3))));
-        value_at[j] = t * value_pitch + unsigned(col) * unsigned(sizeof(T));
-    }
+    for (int l = 0; l < Strip<T>::loads; ++l) value_at[l] = strip_offset<T>(s, pitch_of<T>(s, s.H, s.dv), col >> 4, lane, l);
 
     f32x4 S[kCt];
 #pragma unroll
@@ -203,57 +242,60 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
             for (int i = 0; i < 4; ++i) S[ct][i] = load4(from0, state_offset(s, ct, i, g, col));
     }
 
+    const int first = chunk_at(s, 0), move = s.reverse ? -1 : 1;
+    Walk kr = walk_rows(a.k, s, at.b, at.hk, s.Hk, s.dk, first, move), vr = walk_rows(a.v, s, at.b, at.h, s.H, s.dv, first, move),
+         ws = walk_blocks(ws_all, Ws::bytes, first, move), kw = walk_blocks(kw_all, Kw::bytes, first, move);
     In fk[4][kKs], fkt[kCt][2];
     Mid ft[kTriBlocks];
-    T v[16];
-    auto ws_of = [&](int chunk) __attribute__((always_inline)) { return whole(ws_all + size_t(chunk) * Ws::bytes); };
-    auto load_keys = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc kr = chunk_rows(a.k, s, at.b, at.hk, s.Hk, s.dk, chunk);
+    Strip<T> v;
+    u32x4 raw;
+    auto load_keys = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = kr.here();
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
-            for (int m = 0; m < 4; ++m) load_row(fk[m][ks], kr, key_at[m] + 32u * unsigned(ks * sizeof(T)));
+            for (int m = 0; m < 4; ++m) load_row(fk[m][ks], from0, key_at[m] + 32u * unsigned(ks * sizeof(T)));
     };
-    auto load_values = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc vr = chunk_rows(a.v, s, at.b, at.h, s.H, s.dv, chunk);
+    auto load_first = [&]() __attribute__((always_inline)) {
+        raw = request_scalars(ws.here(), lane);
+        const Rsrc from0 = vr.here();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = load_element<T>(vr, value_at[j]);
+        for (int l = 0; l < Strip<T>::loads; ++l) v.w[l] = load16(from0, value_at[l]);
     };
-    auto load_inverse = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc ws = ws_of(chunk);
+    auto load_inverse = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = ws.here();
 #pragma unroll
-        for (int i = 0; i < kTriBlocks; ++i) ft[i] = get<Mid>(ws, Ws::inverse, i, lane);
+        for (int i = 0; i < kTriBlocks; ++i) ft[i] = get<Mid>(from0, Ws::inverse, i, lane);
     };
-    auto load_transposed = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc kw = whole(kw_all + size_t(chunk) * Kw::bytes);
+    auto load_transposed = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = kw.here();
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int ct = 0; ct < kCt; ++ct) fkt[ct][ks] = get<In>(kw, 0, 2 * ct + ks, lane);
+            for (int ct = 0; ct < kCt; ++ct) fkt[ct][ks] = get<In>(from0, 0, 2 * ct + ks, lane);
     };
     // (in the order of the loop: its waits count the requests behind the one they are for, and hold for the way into the loop as well)
-    u32x4 raw = request_scalars(ws_of(chunk_at(s, 0)), lane);
+    load_first();
     requests_stay();
-    load_keys(chunk_at(s, 0));
+    load_keys();
     requests_stay();
-    load_values(chunk_at(s, 0));
+    load_inverse();
     requests_stay();
-    load_inverse(chunk_at(s, 0));
-    requests_stay();
-    load_transposed(chunk_at(s, 0));
+    load_transposed();
     requests_stay();
 
     for (int step = 0; step < s.chunks; ++step) {
-        const int chunk = chunk_at(s, step), next = step + 1 < s.chunks ? chunk_at(s, step + 1) : chunk;
+        if (step + 1 < s.chunks) kr.next(), vr.next(), ws.next(), kw.next();  // what is requested from here on
         unsigned char *hand = lds + (step & 1) * (kBwd ? Tile<DK>::bytes + Tile<kC>::bytes : Hand::bytes);
         if constexpr (kBwd) {
             __syncthreads();
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) tile_put<DK>(hand, ct, r, g, S[ct]);
         }
+        strip_put(scal + kScalarBytes, v, lane);
         share_scalars(scal, raw, lane);
         requests_stay();
-        raw = request_scalars(ws_of(next), lane);
+        load_first();
         requests_stay();
         Mid fs[kKs];
 #pragma unroll
@@ -269,17 +311,19 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
 #pragma unroll
             for (int m = 0; m < 4; ++m) mma(e[m], fk[m][ks], fs[ks]);
         requests_stay();
-        load_keys(next);
+        load_keys();
         requests_stay();
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const f32x4 c = scalars(scal, kC0, m, g);
+        for (int p = 0; p < 2; ++p) {
+            T x[8];
+            strip_column(x, scal + kScalarBytes, p, r, g);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[m][i] = fmaf(-c[i], e[m][i], value(v[4 * m + i]));
+            for (int j = 0; j < 2; ++j) {
+                const f32x4 c = scalars(scal, kC0, 2 * p + j, g);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[2 * p + j][i] = fmaf(-c[i], e[2 * p + j][i], value(x[4 * j + i]));
+            }
         }
-        requests_stay();
-        load_values(next);
-        requests_stay();
         const Mid fe[2] = {from<Mid>(e[0], e[1]), from<Mid>(e[2], e[3])};
 #pragma unroll
         for (int m = 0; m < 4; ++m) e[m] = zero;
@@ -288,7 +332,7 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
 #pragma unroll
             for (int m = 2 * ks; m < 4; ++m) mma(e[m], ft[lower_block(m, ks)], fe[ks]);
         requests_stay();
-        load_inverse(next);
+        load_inverse();
         requests_stay();
         if constexpr (kBwd) {
 #pragma unroll
@@ -309,7 +353,7 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) mma(S[ct], fkt[ct][ks], fd[ks]);
         requests_stay();
-        load_transposed(next);
+        load_transposed();
         requests_stay();
         if constexpr (!kBwd) __syncthreads();
     }
@@ -331,12 +375,16 @@ __device__ __forceinline__ void emit_states(const ChainArgs<T> &a, const Columns
     const Shape &s = a.s;
     const int part = at.col >> 4;
     const size_t state_bytes = emitted_bytes<T>(DK / 16, s.dv), token_bytes = emitted_bytes<T>(4, s.dv);
+    const int first = chunk_at(s, 0), move = s.reverse ? -1 : 1;
+    const size_t units = size_t(at.slab) * s.chunks;
+    Walk ws = walk_blocks(a.states + units * state_bytes, state_bytes, first, move), we = walk_blocks(a.wrong + units * token_bytes, token_bytes, first, move);
     for (int step = 0; step <= s.chunks; ++step) {
         __syncthreads();
         if (step == 0) continue;
         const unsigned char *hand = lds + ((step - 1) & 1) * (Tile<DK>::bytes + Tile<kC>::bytes);
-        const size_t unit = size_t(at.slab) * s.chunks + chunk_at(s, step - 1);
-        const Rsrc to = whole(a.states + unit * state_bytes), te = whole(a.wrong + unit * token_bytes);
+        const Rsrc to = ws.here(), te = we.here();
+        ws.next();
+        we.next();
         float x[8];
 #pragma unroll
         for (int i = 0; i < DK / 32; ++i) {
@@ -355,7 +403,7 @@ __device__ __forceinline__ void emit_states(const ChainArgs<T> &a, const Columns
 
 // The outputs of a wave's columns, one chunk behind the chain
 template <typename T, int DK, int N>
-__device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at, const unsigned char *lds)
+__device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at, unsigned char *own /* the wave's: scalars, then a tile */, const unsigned char *lds)
 {
     using In = typename operands<T, N>::In;
     using Mid2 = typename operands<T, 2>::Mid;
@@ -364,39 +412,44 @@ __device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at
     constexpr int kKs = DK / 32;
     const Shape &s = a.s;
     const int lane = at.lane, r = at.r, g = at.g;
-    const unsigned char *ws_all = a.ws + size_t(at.slab) * s.chunks * Ws::bytes;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk), value_pitch = pitch_of<T>(s, s.H, s.dv);
-    unsigned key_at[4], value_at[16];
+    unsigned key_at[4], out_at[2];
 #pragma unroll
     for (int m = 0; m < 4; ++m) key_at[m] = row_offset<T>(key_pitch, token_at(s, paired(m, r)), 0, g, s.dk);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) value_at[j] = unsigned(token_at(s, paired(j >> 2, 4 * g + (j & 3)))) * value_pitch + unsigned(at.col) * unsigned(sizeof(T));
+    for (int i = 0; i < 2; ++i)  // the rows that a lane writes, eight columns each
+        out_at[i] = unsigned(token_at(s, 32 * i + (lane >> 1))) * value_pitch + unsigned((at.col & ~15) + 8 * (lane & 1)) * unsigned(sizeof(T));
 
+    const int first = chunk_at(s, 0), move = s.reverse ? -1 : 1;
+    Walk qr = walk_rows(a.q, s, at.b, at.hk, s.Hk, s.dk, first, move), to = walk_rows(static_cast<const T *>(a.out), s, at.b, at.h, s.H, s.dv, first, move),
+         ws = walk_blocks(a.ws + size_t(at.slab) * s.chunks * Ws::bytes, Ws::bytes, first, move);
     In fq[4][kKs];
     Mid2 fp[kTriBlocks];
-    f32x4 c[4];
-    auto load_queries = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc qr = chunk_rows(a.q, s, at.b, at.hk, s.Hk, s.dk, chunk);
+    u32x4 raw;
+    auto load_queries = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = qr.here();
+        raw = request_scalars(ws.here(), lane);
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
-            for (int m = 0; m < 4; ++m) load_row(fq[m][ks], qr, key_at[m] + 32u * unsigned(ks * sizeof(T)));
+            for (int m = 0; m < 4; ++m) load_row(fq[m][ks], from0, key_at[m] + 32u * unsigned(ks * sizeof(T)));
     };
-    auto load_scores = [&](int chunk) __attribute__((always_inline)) {
-        const Rsrc ws = whole(ws_all + size_t(chunk) * Ws::bytes);
+    auto load_scores = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = ws.here();
 #pragma unroll
-        for (int m = 0; m < 4; ++m) c[m] = as_floats(load16(ws, 32u * unsigned(g), 128u * unsigned(m >> 1) + 16u * unsigned(m & 1)));
-#pragma unroll
-        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid2>(ws, Ws::scores, i, lane);
+        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid2>(from0, Ws::scores, i, lane);
     };
-    load_queries(chunk_at(s, 0));
+    load_queries();
     requests_stay();
-    load_scores(chunk_at(s, 0));
+    load_scores();
     requests_stay();
     for (int step = 0; step < s.chunks; ++step) {
-        const int chunk = chunk_at(s, step), next = step + 1 < s.chunks ? chunk_at(s, step + 1) : chunk;
+        const Rsrc out = to.here();
+        to.next();
+        if (step + 1 < s.chunks) qr.next(), ws.next();
         const unsigned char *hand = lds + (step & 1) * Hand::bytes;
+        share_scalars(own, raw, lane);
         __syncthreads();  // the chain has left this chunk's state and u; it writes the other half until the next one
         f32x4 o[4], u[4];
 #pragma unroll
@@ -411,35 +464,41 @@ __device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at
             for (int m = 0; m < 4; ++m) mma(o[m], fq[m][ks], fs);
         }
         requests_stay();
-        load_queries(next);
+        load_queries();
         requests_stay();
         const Mid2 fu[2] = {from<Mid2>(u[0], u[1]), from<Mid2>(u[2], u[3])};
 #pragma unroll
-        for (int m = 0; m < 4; ++m) o[m] *= c[m];
+        for (int m = 0; m < 4; ++m) o[m] *= scalars(own, kC0, m, g);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
             for (int m = 2 * ks; m < 4; ++m) mma(o[m], fp[lower_block(m, ks)], fu[ks]);
         requests_stay();
-        load_scores(next);
+        load_scores();
         requests_stay();
-        const Rsrc to = chunk_rows(a.out, s, at.b, at.h, s.H, s.dv, chunk);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) store_element<T>(to, value_at[j], o[j >> 2][j & 3]);
+        for (int m = 0; m < 4; ++m) tile_put<kC>(own + kScalarBytes, m, r, g, o[m]);
+        wave_fence();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float x[8];
+            tile_row<kC>(x, own + kScalarBytes, 32 * i + (lane >> 1), lane & 1);
+            store_row(out, out_at[i], x, T{});
+        }
     }
 }
 
 // Two waves per 16 columns: the chain, and the outputs one chunk behind it
 template <typename T, int DK, int N>
-__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(1, 1))) void gd_states(ChainArgs<T> a)
+__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(DK <= 64 ? 2 : 1, DK <= 64 ? 2 : 1))) void gd_states(ChainArgs<T> a)
 {
-    __shared__ __align__(16) unsigned char lds[2 * HandOver<T, DK>::bytes], scal[kScalarBytes];
+    __shared__ __align__(16) unsigned char lds[2 * HandOver<T, DK>::bytes], scal[kScalarBytes + Strip<T>::bytes], own[kScalarBytes + Tile<kC>::bytes];
     Columns at;
     if (!columns_of(a.s, at)) return;
     if (threadIdx.x < 64)
         states<T, DK, N, false>(a, at, scal, lds);
     else
-        outputs<T, DK, N>(a, at, lds);
+        outputs<T, DK, N>(a, at, own, lds);
 }
 
 }  // namespace gd
