@@ -338,18 +338,20 @@ struct GradientArgs {
     const unsigned char *key_ws;
 };
 
-// the tokens 4g .. 4g + 3 of the four-token groups of strip w in the lanes of a transposed fragment: channel r
-__device__ __forceinline__ f32x4 four_tokens(const Whole &, Rsrc keys, size_t first, int block, int w, int r, int g)
+// the tokens 16 w + 4g .. + 3 of channel r in a transposed fragment in LDS
+__device__ __forceinline__ f32x4 four_tokens(const Whole &, const unsigned char *lds, int block, int w, int r, int g)
 {
-    const unsigned lane = unsigned(r + 16 * (2 * (w & 1) + (g >> 1)));
-    const u32x2 u = __builtin_amdgcn_raw_buffer_load_b64(keys, 16u * lane + 8u * unsigned(g & 1), unsigned(first) + unsigned(block) * 1024u, 0);
-    return unpack4(make_uint2(u[0], u[1]));
+    const int lane = r + 16 * (2 * (w & 1) + (g >> 1));
+    return unpack4(*reinterpret_cast<const uint2 *>(lds + block * 1024 + 16 * lane + 8 * (g & 1)));
 }
-__device__ __forceinline__ f32x4 four_tokens(const Full &, Rsrc keys, size_t first, int block, int w, int r, int g)
+__device__ __forceinline__ f32x4 four_tokens(const Full &, const unsigned char *lds, int block, int w, int r, int g)
 {
-    const unsigned lane = unsigned(r + 16 * (2 * (w & 1) + (g >> 1)));
-    return as_floats(load16(keys, 16u * lane + 1024u * unsigned(g & 1), unsigned(first) + unsigned(block) * 2048u));
+    const int lane = r + 16 * (2 * (w & 1) + (g >> 1));
+    return *reinterpret_cast<const f32x4 *>(lds + block * 2048 + 1024 * (g & 1) + 16 * lane);
 }
+
+__device__ __forceinline__ void lds_element(bf16_t *p, float x) { p->bits = uint16_t(pack2(x, x)); }
+__device__ __forceinline__ void lds_element(float *p, float x) { *p = x; }
 
 // a fragment at a lane's offset (0, or nowhere for one that is not there)
 template <typename Frag>
@@ -382,34 +384,68 @@ __device__ __forceinline__ float dot(const Full &a, const Full &b, float acc)
     return acc;
 }
 
-// One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  The contractions over value columns take kSlice of them
-// at a time: e and the rows of S and D, which all waves need, are split once and shared through LDS; afterwards X and Y take the states' place.
-template <typename T, int DK>
-__global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientArgs<T> a)
+// One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  What more than one wave needs -- rows of k, K^T and Q^T, e,
+// the rows of S and D -- each requests a quarter of and all read from LDS; every request of a turn stands before its first wait, since a workgroup's
+// time is mostly that of its trips to memory.  The contractions over value columns take kSlice of them at a time.
+// kOne: the values are one slice; two workgroups then fit a compute unit's registers (without it the accumulators are live across the
+// requests of the next slice, and what spills costs more than the second workgroup brings).
+template <typename T, int DK, bool kOne>
+__global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) void gd_gradients(GradientArgs<T> a)
 {
     using In = typename operands<T, 2>::In;
     using Mid = typename operands<T, 2>::Mid;
     using Kw = KeyWs<T, DK, true>;
     constexpr int kKs = DK / 32, kCt = DK / 16, kSlice = DK <= 64 ? 64 : 32, kVs = kSlice / 32;
-    constexpr int kStates = 2 * kCt * kVs * int(frag_bytes<Mid>), kTiles = 2 * kC * kPitch * 4;
-    __shared__ __align__(16) unsigned char shared[kStates > kTiles ? kStates : kTiles], wrong[4 * kVs * frag_bytes<Mid>];
-    __shared__ double sum[kC];
-    __shared__ float bet[kC], enters[kC], leaves[kC], pairs[4][kC], through[4];
+    constexpr int kStates = 2 * kCt * kVs * int(frag_bytes<Mid>), kTiles = 2 * kC * kPitch * 4, kOwn = (kCt * kVs + 3) / 4;
+    extern __shared__ __align__(16) unsigned char shared[];  // the rows of S and D, afterwards X and Y; then what is below
+    unsigned char *wrong = shared + (kStates > kTiles ? kStates : kTiles), *key_rows = wrong + 4 * kVs * frag_bytes<Mid>,
+                  *key_columns = key_rows + 4 * kKs * frag_bytes<In>;
+    __shared__ double sum[4][kC];
+    __shared__ float bet[4][kC], enters[kC], leaves[kC], pairs[4][kC], through[4];
     float *X = reinterpret_cast<float *>(shared), *Y = X + kC * kPitch;
     unsigned char *fS = shared, *fD = shared + kStates / 2;
     const Shape &s = a.s;
-    const int w = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
+    int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const unsigned unit = blockIdx.x, key_slab = unit / unsigned(s.chunks);
     const int chunk = int(unit - key_slab * unsigned(s.chunks));
     const int b = int(key_slab / unsigned(s.Hk)), hk = int(key_slab - unsigned(b) * unsigned(s.Hk)), share = s.H / s.Hk;
-    const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk);
+    const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk), value_pitch = pitch_of<T>(s, s.H, s.dv);
     const Rsrc kw = whole(a.key_ws + size_t(unit) * Kw::bytes);
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    const int blocks = value_blocks(s.dv);
+    const size_t state_bytes = emitted_bytes<T>(kCt, s.dv), token_bytes = emitted_bytes<T>(4, s.dv);
 
-    f32x4 qk[4], kk[4], dq[kCt], dk[kCt];
+    Gates<T, true> gates;
+    In fo[kVs];
+    Mid fr[kVs], fe[kVs], fs[kOwn], fd[kOwn];
+    auto request_gates = [&](int h) __attribute__((always_inline)) { gates.request(a.g, a.beta, s, b, h, chunk, lane); };
+    auto request_slice = [&](int h, int v0) __attribute__((always_inline)) {
+        const size_t value_unit = (size_t(b) * s.H + h) * s.chunks + unsigned(chunk);
+        const Rsrc dor = chunk_rows(a.d_out, s, b, h, s.H, s.dv, chunk), er = whole(a.wrong + value_unit * token_bytes),
+                   rr = whole(a.r + value_unit * token_bytes), Sr = whole(a.states + value_unit * state_bytes),
+                   Dr = whole(a.adjoints + value_unit * state_bytes);
+#pragma unroll
+        for (int ks = 0; ks < kVs; ++ks) {
+            const unsigned nowhere = v0 + ks < blocks ? 0u : kNowhere;
+            load_row(fo[ks], dor, row_offset<T>(value_pitch, token_at(s, 16 * w + r), v0 + ks, g, s.dv));
+            fe[ks] = get_at<Mid>(er, nowhere, w * blocks + v0 + ks, lane);
+            fr[ks] = get_at<Mid>(rr, nowhere, w * blocks + v0 + ks, lane);
+        }
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o) {
+            const int block = 4 * o + w, ct = block / kVs, ks = block % kVs;
+            const unsigned nowhere = block < kCt * kVs && v0 + ks < blocks ? 0u : kNowhere;
+            fs[o] = get_at<Mid>(Sr, nowhere, ct * blocks + v0 + ks, lane);
+            fd[o] = get_at<Mid>(Dr, nowhere, ct * blocks + v0 + ks, lane);
+        }
+    };
+
+    f32x4 dq[kCt], dk[kCt];
+    In fq[kKs], fk[kKs], fkc[Kw::blocks / 2];
     {
         const Rsrc qr = chunk_rows(a.q, s, b, hk, s.Hk, s.dk, chunk), kr = chunk_rows(a.k, s, b, hk, s.Hk, s.dk, chunk);
-        In fq[kKs], fk[kKs];
+        request_gates(hk * share);
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) {
             const unsigned at = row_offset<T>(key_pitch, token_at(s, 16 * w + r), ks, g, s.dk);
@@ -417,75 +453,60 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
             load_row(fk[ks], kr, at);
         }
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            qk[n] = kk[n] = zero;
-            if (n > w) continue;
-#pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) {
-                In fb;
-                load_row(fb, kr, row_offset<T>(key_pitch, token_at(s, 16 * n + r), ks, g, s.dk));
-                mma(qk[n], fq[ks], fb);
-                mma(kk[n], fk[ks], fb);
-            }
-        }
+        for (int o = 0; o < Kw::blocks / 2; ++o) fkc[o] = get<In>(kw, 0, 4 * o + w, lane);  // K^T, then Q^T
+        request_slice(hk * share, 0);
+        requests_stay();
     }
+#pragma unroll
+    for (int ks = 0; ks < kKs; ++ks) lds_put(key_rows, w * kKs + ks, lane, fk[ks]);
+#pragma unroll
+    for (int o = 0; o < Kw::blocks / 2; ++o) lds_put(key_columns, 4 * o + w, lane, fkc[o]);
 #pragma unroll
     for (int ct = 0; ct < kCt; ++ct) dq[ct] = dk[ct] = zero;
 
     for (int h = hk * share; h < (hk + 1) * share; ++h) {
-        const size_t slab = size_t(b) * s.H + h, value_unit = slab * s.chunks + unsigned(chunk);
-        const size_t state_bytes = emitted_bytes<T>(kCt, s.dv), token_bytes = emitted_bytes<T>(4, s.dv);
-        const Rsrc dor = chunk_rows(a.d_out, s, b, h, s.H, s.dv, chunk), er = whole(a.wrong + value_unit * token_bytes),
-                   rr = whole(a.r + value_unit * token_bytes), Sr = whole(a.states + value_unit * state_bytes),
-                   Dr = whole(a.adjoints + value_unit * state_bytes);
-        const int blocks = value_blocks(s.dv);
-        const unsigned own = unsigned(token_at(s, 16 * w + r));
-        if (w == 0) {
-            const Rsrc gr = chunk_rows(a.g, s, b, h, s.H, 1, chunk), br = chunk_rows(a.beta, s, b, h, s.H, 1, chunk);
-            const unsigned at = unsigned(token_at(s, lane)) * pitch_of<T>(s, s.H, 1);
-            sum[lane] = wave_prefix(double(fmaxf(value(load_element<T>(gr, at)), kGateFloor)), lane);
-            bet[lane] = beta_divisor(value(load_element<T>(br, at)));
-        }
+        // (addresses are formed from here on in every turn: formed once for all, they would be more than the registers hold)
+        asm volatile("" : "+v"(lane));
+        r = lane & 15, g = lane >> 4;
         f32x4 x[4], y[4], read[kCt], erase[kCt], write[kCt];
 #pragma unroll
         for (int n = 0; n < 4; ++n) x[n] = y[n] = zero;
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) read[ct] = erase[ct] = write[ct] = zero;
+        if (h > hk * share) {
+            request_gates(h);
+            request_slice(h, 0);
+            requests_stay();
+        }
+        sum[w][lane] = gates.sum(lane);
+        bet[w][lane] = gates.strength();
         float ds = 0.f;  // <D, S>
-        for (int v0 = 0; v0 < blocks; v0 += kVs) {
-            In fo[kVs];
-            Mid fr[kVs], fe[kVs];
-#pragma unroll
-            for (int ks = 0; ks < kVs; ++ks) {
-                const bool has = v0 + ks < blocks;
-                load_row(fo[ks], dor, row_offset<T>(pitch_of<T>(s, s.H, s.dv), int(own), v0 + ks, g, s.dv));
-                const unsigned nowhere = has ? 0u : kNowhere;
-                fe[ks] = get_at<Mid>(er, nowhere, w * blocks + v0 + ks, lane);
-                fr[ks] = get_at<Mid>(rr, nowhere, w * blocks + v0 + ks, lane);
-                lds_put(wrong, w * kVs + ks, lane, fe[ks]);
+        for (int v0 = 0; v0 < (kOne ? 1 : blocks); v0 += kVs) {
+            if (!kOne && v0 > 0) {
+                request_slice(h, v0);
+                requests_stay();
             }
 #pragma unroll
-            for (int o = 0; o < (kCt * kVs + 3) / 4; ++o) {
-                const int block = 4 * o + w, ct = block / kVs, ks = block % kVs;
-                if (kCt * kVs % 4 != 0 && block >= kCt * kVs) break;
-                const unsigned nowhere = v0 + ks < blocks ? 0u : kNowhere;
-                const Mid fs = get_at<Mid>(Sr, nowhere, ct * blocks + v0 + ks, lane), fd = get_at<Mid>(Dr, nowhere, ct * blocks + v0 + ks, lane);
-                ds = dot(fs, fd, ds);
-                lds_put(fS, block, lane, fs);
-                lds_put(fD, block, lane, fd);
-            }
+            for (int ks = 0; ks < kVs; ++ks) lds_put(wrong, w * kVs + ks, lane, fe[ks]);
+#pragma unroll
+            for (int o = 0; o < kOwn; ++o)
+                if (kCt * kVs % 4 == 0 || 4 * o + w < kCt * kVs) {
+                    ds = dot(fs[o], fd[o], ds);
+                    lds_put(fS, 4 * o + w, lane, fs[o]);
+                    lds_put(fD, 4 * o + w, lane, fd[o]);
+                }
             __syncthreads();
 #pragma unroll
             for (int ks = 0; ks < kVs; ++ks) {
 #pragma unroll
-                for (int n = 0; n < 4; ++n)
-                    if (n <= w) {
-                        const Mid f = n == w ? fe[ks] : lds_get<Mid>(wrong, n * kVs + ks, lane);
-                        mma(x[n], fo[ks], f);
-                        mma(y[n], fr[ks], f);
-                    }
+                for (int n = 0; n < 4; ++n) {  // (the upper tiles too: the last wave has all four, and branches cost the others more)
+                    const Mid f = lds_get<Mid>(wrong, n * kVs + ks, lane);
+                    mma(x[n], fo[ks], f);
+                    mma(y[n], fr[ks], f);
+                }
 #pragma unroll
                 for (int ct = 0; ct < kCt; ++ct) {
+                    if (ct % 2 == 0) requests_stay();  // (fragments from LDS: two tiles' ahead, not all)
                     const Mid f = lds_get<Mid>(fS, ct * kVs + ks, lane);
                     mma(read[ct], fo[ks], f);
                     mma(erase[ct], fr[ks], f);
@@ -498,28 +519,36 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
         if (lane == 0) through[w] = ds;
 
         // X, Y and the pairs' part of dg
-        const Rsrc dbr = chunk_rows(a.dbeta, s, b, h, s.H, 1, chunk);
+        {  // r_t . e_t stands on the diagonal of y
+            const f32x4 d = w < 2 ? (w == 0 ? y[0] : y[1]) : (w == 2 ? y[2] : y[3]);
+            const float db = (r & 2) ? ((r & 1) ? d[3] : d[2]) : ((r & 1) ? d[1] : d[0]);
+            store_element<T>(chunk_rows(a.dbeta, s, b, h, s.H, 1, chunk), (r >> 2) == g ? unsigned(token_at(s, 16 * w + r)) * pitch_of<T>(s, s.H, 1) : kNowhere, db);
+        }
         float carry[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             float column = 0.f;
             const int c = 16 * n + r;
+            f32x4 qk = zero, kk = zero;
+            requests_stay();
+#pragma unroll
+            for (int ks = 0; ks < kKs; ++ks) {
+                const In f = lds_get<In>(key_rows, n * kKs + ks, lane);
+                mma(qk, fq[ks], f);
+                mma(kk, fk[ks], f);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int t = 16 * w + 4 * g + i;
-                float xi = 0.f, yi = 0.f;
-                if (n == w && r == 4 * g + i)  // r_t . e_t
-                    store_element<T>(dbr, unsigned(token_at(s, t)) * pitch_of<T>(s, s.H, 1), y[n][i]);
-                if (n <= w) {
-                    const float decay = c <= t ? expf(float(sum[t] - sum[c])) * bet[c] : 0.f;
-                    xi = decay * x[n][i];
-                    yi = c < t ? -decay * bet[t] * y[n][i] : 0.f;
-                    const float z = c < t ? xi * qk[n][i] + yi * kk[n][i] : 0.f, upto = row_scan<0>(z);
-                    column += c <= t ? upto - z + carry[i] : 0.f;  // pairs (t, i < c)
-                    carry[i] += __shfl(upto, lane | 15);
-                }
+                // (factors of 0 and 1 rather than branches)
+                const float upto_t = c <= t ? 1.f : 0.f, before_t = c < t ? 1.f : 0.f;
+                const float decay = exp2_of(c <= t ? sum[w][t] - sum[w][c] : 0.0) * bet[w][c];
+                const float xi = upto_t * decay * x[n][i], yi = before_t * -decay * bet[w][t] * y[n][i];
                 X[t * kPitch + c] = xi;
                 Y[t * kPitch + c] = yi;
+                const float z = before_t * xi * qk[i] + yi * kk[i], upto = row_scan<0>(z);
+                column += upto_t * (upto - z + carry[i]);  // pairs (t, i < c)
+                carry[i] += __shfl(upto, lane | 15);
             }
             column += __shfl_xor(column, 16);
             column += __shfl_xor(column, 32);
@@ -529,18 +558,19 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * w + 4 * g + i;
-            const float c = expf(float(sum[t])), d = expf(float(sum[kC - 1] - sum[t])) * bet[t];
+            const float c = exp2_of(sum[w][t]), d = exp2_of(sum[w][kC - 1] - sum[w][t]) * bet[w][t];
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) {
                 read[ct][i] *= c;
-                erase[ct][i] *= -c * bet[t];
+                erase[ct][i] *= -c * bet[w][t];
                 write[ct][i] *= d;
             }
         }
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) {
-            const f32x4 qe = four_tokens(In{}, kw, Kw::blocks * frag_bytes<In>, 2 * ct + (w >> 1), w, r, g);
-            const f32x4 ke = four_tokens(In{}, kw, 0, 2 * ct + (w >> 1), w, r, g);
+            if (ct % 2 == 0) requests_stay();
+            const f32x4 qe = four_tokens(In{}, key_columns, Kw::blocks + 2 * ct + (w >> 1), w, r, g);
+            const f32x4 ke = four_tokens(In{}, key_columns, 2 * ct + (w >> 1), w, r, g);
             enter += qe * read[ct] + ke * erase[ct];
             leave += ke * write[ct];
             dq[ct] += read[ct];
@@ -569,7 +599,8 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
             make(fy, y8);
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) {
-                const In fkt = get<In>(kw, 0, 2 * ct + ks, lane), fqt = get<In>(kw, Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
+                if (ct % 2 == 0) requests_stay();
+                const In fkt = lds_get<In>(key_columns, 2 * ct + ks, lane), fqt = lds_get<In>(key_columns, Kw::blocks + 2 * ct + ks, lane);
                 mma(dq[ct], fx, fkt);
                 mma(dk[ct], ft, fqt);
                 mma(dk[ct], fy, fkt);
@@ -585,7 +616,7 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
             }
             const float earlier = __shfl_up(before, 1);
             before = lane > 0 ? earlier : 0.f;
-            const float state = expf(float(sum[kC - 1])) * ((through[0] + through[1]) + (through[2] + through[3]));
+            const float state = exp2_of(sum[w][kC - 1]) * ((through[0] + through[1]) + (through[2] + through[3]));
             const float dg = after + before + ((pairs[0][lane] + pairs[1][lane]) + (pairs[2][lane] + pairs[3][lane])) + state;
             store_element<T>(chunk_rows(a.dg, s, b, h, s.H, 1, chunk), unsigned(token_at(s, lane)) * pitch_of<T>(s, s.H, 1), dg);
         }
@@ -600,7 +631,7 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) io<T>::store(rows + (4 * g + i) * kRowPitch + paired(ct, r), which == 0 ? dq[ct][i] : dk[ct][i]);
+            for (int i = 0; i < 4; ++i) lds_element(rows + (4 * g + i) * kRowPitch + paired(ct, r), which == 0 ? dq[ct][i] : dk[ct][i]);
         wave_fence();
         constexpr int kPiece = 16 / int(sizeof(T)), kPieces = DK / kPiece;
 #pragma unroll
@@ -611,6 +642,16 @@ __global__ __launch_bounds__(256, DK <= 64 ? 2 : 1) void gd_gradients(GradientAr
         }
         wave_fence();
     }
+}
+
+template <typename T, int DK>
+constexpr size_t gradient_lds()
+{
+    constexpr int vs = DK <= 64 ? 2 : 1;
+    using In = typename operands<T, 2>::In;
+    using Mid = typename operands<T, 2>::Mid;
+    constexpr size_t states = 2 * DK / 16 * vs * frag_bytes<Mid>, tiles = 2 * kC * kPitch * 4;
+    return (states > tiles ? states : tiles) + 4 * vs * frag_bytes<Mid> + 4 * DK / 32 * frag_bytes<In> + KeyWs<T, DK, true>::bytes;
 }
 
 struct Buffers {
@@ -648,7 +689,11 @@ hipError_t launch(const Shape &s, const GradientPointers &p, void *workspace, hi
     gd_prepare<T, DK, N, true><<<slabs * unsigned(s.chunks), 256, 0, stream>>>(prepare);
     gd_both_chains<T, DK, N><<<dim3((slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 2), 128, 0, stream>>>(chain, adjoint);
     const unsigned key_units = unsigned(s.B) * unsigned(s.Hk) * unsigned(s.chunks);
-    gd_gradients<T, DK><<<key_units, 256, 0, stream>>>(gradient);
+    constexpr size_t lds = gradient_lds<T, DK>();
+    if (s.dv <= (DK <= 64 ? 64 : 32))
+        gd_gradients<T, DK, true><<<key_units, 256, lds, stream>>>(gradient);
+    else
+        gd_gradients<T, DK, false><<<key_units, 256, lds, stream>>>(gradient);
     return hipGetLastError();
 }
 

@@ -43,66 +43,143 @@ __device__ __forceinline__ double wave_prefix(double x, int lane)
     return x;
 }
 
+// Sums of the gates up to each token, in scan order and in powers of two, and the strengths: every wave its own (a lane a token).  Differences of
+// the 64-bit sums are rounded to 32 bits where they are exponentiated.
+template <typename T, bool kBwd>
+struct Gates {
+    T g, beta;
+    __device__ __forceinline__ void request(const T *gates, const T *strengths, const Shape &s, int b, int h, int chunk, int lane)
+    {
+        const unsigned at = unsigned(token_at(s, lane)) * pitch_of<T>(s, s.H, 1);
+        g = load_element<T>(chunk_rows(gates, s, b, h, s.H, 1, chunk), at);
+        beta = load_element<T>(chunk_rows(strengths, s, b, h, s.H, 1, chunk), at);
+    }
+    __device__ __forceinline__ double sum(int lane) const
+    {
+        const double kLog2e = 1.4426950408889634074;
+        return wave_prefix(kLog2e * double(fmaxf(value(g), kGateFloor)), lane);
+    }
+    __device__ __forceinline__ float strength() const { return kBwd ? beta_divisor(value(beta)) : value(beta); }
+};
+
+__device__ __forceinline__ float exp2_of(double x) { return fast_exp2(float(x)); }
+
+// Rows of a chunk in LDS, as they are, for fragments of rows and of columns
+template <typename T, int DK>
+struct KeyTile {
+    static constexpr int pitch = DK + (sizeof(T) == 2 ? 8 : 4), bytes = kC * pitch * int(sizeof(T));
+};
+template <typename T, int DK, typename In>
+__device__ __forceinline__ void key_put(unsigned char *lds, int row, int step, int g, const In &f)
+{
+    __builtin_memcpy(lds + (row * KeyTile<T, DK>::pitch + 32 * step + 8 * g) * int(sizeof(T)), &f, sizeof(f));
+}
+template <typename T, int DK, typename In>
+__device__ __forceinline__ void key_get(In &f, const unsigned char *lds, int row, int step, int g)
+{
+    __builtin_memcpy(&f, __builtin_assume_aligned(lds + (row * KeyTile<T, DK>::pitch + 32 * step + 8 * g) * int(sizeof(T)), 16), sizeof(f));
+}
+// channels paired(tile, r), tokens 32 step + 8g .. + 7
+template <int DK>
+__device__ __forceinline__ void key_column(Whole &f, const unsigned char *lds, int tile, int step, int r, int g)
+{
+    const uint16_t *q = reinterpret_cast<const uint16_t *>(lds) + (32 * step + 8 * g + (r >> 2)) * KeyTile<bf16_t, DK>::pitch + paired(tile, 4 * (r & 3));
+    f.v = join(lds_read_tr(q), lds_read_tr(q + 4 * KeyTile<bf16_t, DK>::pitch));
+}
+template <int DK>
+__device__ __forceinline__ void key_column(Full &f, const unsigned char *lds, int tile, int step, int r, int g)
+{
+    const float *q = reinterpret_cast<const float *>(lds) + (32 * step + 8 * g) * KeyTile<float, DK>::pitch + paired(tile, r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f.v[j] = q[j * KeyTile<float, DK>::pitch];
+}
+
 template <typename T, int DK, int N, bool kBwd>
 __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
 {
     using In = typename operands<T, N>::In;
     using Ws = ChunkWs<T, N, kBwd>;
-    constexpr int kKs = DK / 32;
-    __shared__ __align__(16) float inv[kC * kPitch], sco[kC * kPitch];
-    __shared__ double sum[kC];
-    __shared__ float bet[kC];
+    using Kw = KeyWs<T, DK, kBwd>;
+    constexpr int kKs = DK / 32, kTiles = 2 * kC * kPitch * 4, kKeys = KeyTile<T, DK>::bytes * (kBwd ? 2 : 1);
+    __shared__ __align__(16) unsigned char shared[kTiles > kKeys ? kTiles : kKeys];  // rows of k (and q), afterwards the two matrices
+    __shared__ double sum[4][kC];
+    __shared__ float bet[4][kC];
+    float *inv = reinterpret_cast<float *>(shared), *sco = inv + kC * kPitch;
     const Shape &s = a.s;
     const int w = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const unsigned unit = blockIdx.x, slab = unit / unsigned(s.chunks), chunk = unit - slab * unsigned(s.chunks);
+    const unsigned unit = blockIdx.x, slab = unit / unsigned(s.chunks);
+    const int chunk = int(unit - slab * unsigned(s.chunks));
     const int b = int(slab / unsigned(s.H)), h = int(slab - unsigned(b) * unsigned(s.H)), share = s.H / s.Hk, hk = h / share;
-    const Rsrc kr = chunk_rows(a.k, s, b, hk, s.Hk, s.dk, int(chunk)), qr = chunk_rows(a.q, s, b, hk, s.Hk, s.dk, int(chunk));
-    const unsigned pitch = pitch_of<T>(s, s.Hk, s.dk);
     const Rsrc ws = whole(a.ws + size_t(unit) * Ws::bytes);
 
-    // a wave's rows of q and k; columns are the rows of the strips up to its own
-    In fq[kKs], fk[kKs];
+    Gates<T, kBwd> gates;
+    gates.request(a.g, a.beta, s, b, h, chunk, lane);
+    In fq[kKs], fk[kKs];  // a wave's rows
+    {
+        const Rsrc kr = chunk_rows(a.k, s, b, hk, s.Hk, s.dk, chunk), qr = chunk_rows(a.q, s, b, hk, s.Hk, s.dk, chunk);
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+            const unsigned at = row_offset<T>(pitch_of<T>(s, s.Hk, s.dk), token_at(s, 16 * w + r), ks, g, s.dk);
+            load_row(fk[ks], kr, at);
+            load_row(fq[ks], qr, at);
+        }
+    }
+    requests_stay();
+    {
+        const double p = gates.sum(lane), total = __shfl(p, 63);
+        const float beta = gates.strength();
+        sum[w][lane] = p;
+        bet[w][lane] = beta;
+        if (w == 0) {
+            store4(ws, 4u * unsigned(lane), exp2_of(p));
+            store4(ws, 4u * unsigned(lane), beta, 4 * kC);
+            store4(ws, 4u * unsigned(lane), exp2_of(total - p), 8 * kC);
+            if constexpr (kBwd) store4(ws, 4u * unsigned(lane), 1.f / beta, 12 * kC);
+        }
+    }
 #pragma unroll
     for (int ks = 0; ks < kKs; ++ks) {
-        const unsigned at = row_offset<T>(pitch, token_at(s, 16 * w + r), ks, g, s.dk);
-        load_row(fq[ks], qr, at);
-        load_row(fk[ks], kr, at);
+        key_put<T, DK>(shared, 16 * w + r, ks, g, fk[ks]);
+        if constexpr (kBwd) key_put<T, DK>(shared + KeyTile<T, DK>::bytes, 16 * w + r, ks, g, fq[ks]);
     }
-    if (w == 0) {
-        const Rsrc gr = chunk_rows(a.g, s, b, h, s.H, 1, int(chunk)), br = chunk_rows(a.beta, s, b, h, s.H, 1, int(chunk));
-        const unsigned at = unsigned(token_at(s, lane)) * pitch_of<T>(s, s.H, 1);
-        const float gate = fmaxf(value(load_element<T>(gr, at)), kGateFloor);
-        float beta = value(load_element<T>(br, at));
-        if constexpr (kBwd) beta = beta_divisor(beta);
-        const double p = wave_prefix(double(gate), lane), total = __shfl(p, 63);
-        sum[lane] = p;
-        bet[lane] = beta;
-        store4(ws, 4u * unsigned(lane), expf(float(p)));
-        store4(ws, 4u * unsigned(lane), beta, 4 * kC);
-        store4(ws, 4u * unsigned(lane), expf(float(total - p)), 8 * kC);
-        if constexpr (kBwd) store4(ws, 4u * unsigned(lane), 1.f / beta, 12 * kC);
+    __syncthreads();
+    if (h == hk * share) {  // K^T and Q^T once per key head
+        const Rsrc kw = whole(a.key_ws + ((size_t(b) * s.Hk + hk) * s.chunks + chunk) * Kw::bytes);
+#pragma unroll
+        for (int o = 0; o < Kw::blocks / 4; ++o) {
+            const int block = 4 * o + w;
+            In f;
+            key_column<DK>(f, shared, block >> 1, block & 1, r, g);
+            put(kw, 0, block, lane, f);
+            if constexpr (kBwd) {
+                key_column<DK>(f, shared + KeyTile<T, DK>::bytes, block >> 1, block & 1, r, g);
+                put(kw, Kw::blocks * frag_bytes<In>, block, lane, f);
+            }
+        }
+    }
+    f32x4 kk[4], qk[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        kk[n] = qk[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {  // (the upper tiles too: the last wave has all four, and branches cost the others more)
+            In fb;
+            key_get<T, DK>(fb, shared, 16 * n + r, ks, g);
+            mma(kk[n], fk[ks], fb);
+            mma(qk[n], fq[ks], fb);
+        }
     }
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-        f32x4 kk = {0.f, 0.f, 0.f, 0.f}, qk = kk;
-        if (n <= w) {
-#pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) {
-                In fb;
-                load_row(fb, kr, row_offset<T>(pitch, token_at(s, 16 * n + r), ks, g, s.dk));
-                mma(kk, fk[ks], fb);
-                mma(qk, fq[ks], fb);
-            }
-        }
+    for (int n = 0; n < 4; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * w + 4 * g + i, c = 16 * n + r;
-            const float decay = c <= t ? expf(float(sum[t] - sum[c])) : 0.f;
-            inv[t * kPitch + c] = c < t ? decay * bet[c] * kk[i] : 0.f;
-            sco[t * kPitch + c] = c <= t ? decay * qk[i] : 0.f;
+            // (factors of 0 and 1 rather than branches)
+            const float decay = exp2_of(c <= t ? sum[w][t] - sum[w][c] : 0.0);
+            inv[t * kPitch + c] = (c < t ? 1.f : 0.f) * decay * bet[w][c] * kk[n][i];
+            sco[t * kPitch + c] = (c <= t ? 1.f : 0.f) * decay * qk[n][i];
         }
-    }
     __syncthreads();
     {  // diagonal blocks: column r of the inverse of block w
         float *d = inv + 16 * w * kPitch + 16 * w;
@@ -176,28 +253,6 @@ __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
             put(ws, Ws::inverse + kTriBlocks * frag_bytes<Mid>, upper_block(w, ks), lane, f);
             make(f, p);
             put(ws, Ws::scores, upper_block(w, ks), lane, f);
-        }
-    }
-    if (h == hk * share) {  // once per key head
-        using Kw = KeyWs<T, DK, kBwd>;
-        const Rsrc kw = whole(a.key_ws + ((size_t(b) * s.Hk + hk) * s.chunks + chunk) * Kw::bytes);
-#pragma unroll
-        for (int o = 0; o < Kw::blocks / 4; ++o) {
-            const int block = 4 * o + w, tile = block >> 1, ks = block & 1, c = paired(tile, r);
-            T x[8], y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const unsigned at = c < s.dk ? unsigned(token_at(s, 32 * ks + 8 * g + j)) * pitch + unsigned(c) * unsigned(sizeof(T)) : kNowhere;
-                x[j] = load_element<T>(kr, at);
-                if constexpr (kBwd) y[j] = load_element<T>(qr, at);
-            }
-            In f;
-            gather(f, x);
-            put(kw, 0, block, lane, f);
-            if constexpr (kBwd) {
-                gather(f, y);
-                put(kw, Kw::blocks * frag_bytes<In>, block, lane, f);
-            }
         }
     }
 }
