@@ -311,7 +311,7 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
 
 // Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'
 template <typename T, int DK, int N>
-__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(DK <= 64 ? 2 : 1, DK <= 64 ? 2 : 1))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
+__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(chain_waves<T, DK>, chain_waves<T, DK>))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
 {
     __shared__ __align__(16) unsigned char lds[AdjointLds<DK>::bytes], scal[kScalarBytes + Strip<T>::bytes], own[kScalarBytes + Strip<T>::bytes];
     Columns at;

@@ -488,9 +488,13 @@ __device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at
     }
 }
 
+// Waves on a SIMD: two where their registers fit
+template <typename T, int DK>
+constexpr int chain_waves = DK * int(sizeof(T)) <= 128 ? 2 : 1;
+
 // Two waves per 16 columns: the chain, and the outputs one chunk behind it
 template <typename T, int DK, int N>
-__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(DK <= 64 ? 2 : 1, DK <= 64 ? 2 : 1))) void gd_states(ChainArgs<T> a)
+__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(chain_waves<T, DK>, chain_waves<T, DK>))) void gd_states(ChainArgs<T> a)
 {
     __shared__ __align__(16) unsigned char lds[2 * HandOver<T, DK>::bytes], scal[kScalarBytes + Strip<T>::bytes], own[kScalarBytes + Tile<kC>::bytes];
     Columns at;
