@@ -103,6 +103,24 @@ __device__ __forceinline__ Values<T> vector_or(const T *p, int c, float value)
     return x;
 }
 
+// a group's pair for each of a thread's channels: one, where groups are whole pieces
+template <typename T>
+__device__ __forceinline__ void by_group(const float2 *pair, int c, int width, float (&x)[kVec<T>], float (&y)[kVec<T>])
+{
+    if (width % kVec<T> == 0) {
+        const float2 v = pair[c / width];
+#pragma unroll
+        for (int e = 0; e < kVec<T>; ++e) x[e] = v.x, y[e] = v.y;
+    } else {
+#pragma unroll
+        for (int e = 0; e < kVec<T>; ++e) {
+            const float2 v = pair[(c + e) / width];
+            x[e] = v.x;
+            y[e] = v.y;
+        }
+    }
+}
+
 // ---- a group per workgroup -------------------------------------------------------------------------
 
 template <typename T, int R /* pieces of a thread */, bool kSilu>
@@ -208,23 +226,27 @@ __global__ __launch_bounds__(kThreads) void norm_strip_kernel(NormArgs<T> a)
                 entry[rg * p.C + vec * V + e] = make_float2(fmaf(s1[e], inv, base.v[e]), fmaxf(fmaf(-s1[e] * inv, s1[e], s2[e]), 0.f));
         }
     __syncthreads();
-    const int lane = threadIdx.x & 63, width = p.C / p.G, entries = p.row_groups * width;
+    const int lane = threadIdx.x & 63, width = p.C / p.G;
     for (int j = threadIdx.x >> 6; j < p.G; j += kThreads / 64) {
-        float sum = 0.f;
-        for (int i = lane; i < entries; i += 64) {
-            const int g = i / width, c = i - g * width;
-            sum = fmaf(float(rows_of_group(rows, g, p.row_groups)), entry[g * p.C + j * width + c].x, sum);
+        const float2 *own = entry + j * width;
+        const float mean0 = own[0].x;  // distances from one of the means: sums of them lose nothing
+        float s1 = 0.f, s2 = 0.f;
+        for (int g = 0; g < p.row_groups; ++g) {
+            const float n = float(rows_of_group(rows, g, p.row_groups));
+            if (n > 0.f)
+                for (int c = lane; c < width; c += 64) {
+                    const float2 v = own[g * p.C + c];
+                    const float d = v.x - mean0;
+                    s1 = fmaf(n, d, s1);
+                    s2 += fmaf(n * d, d, v.y);
+                }
         }
-        const float mean = wave_sum(sum) / (float(rows) * float(width));
-        float sq = 0.f;
-        for (int i = lane; i < entries; i += 64) {
-            const int g = i / width, c = i - g * width;
-            const float2 v = entry[g * p.C + j * width + c];
-            const float d = v.x - mean;
-            sq += fmaf(float(rows_of_group(rows, g, p.row_groups)) * d, d, v.y);
+        s1 = wave_sum(s1);
+        s2 = wave_sum(s2);
+        if (lane == 0) {
+            const float all = float(rows) * float(width);
+            a.partial[size_t(blockIdx.x) * p.G + j] = make_float2(mean0 + s1 / all, fmaxf(s2 - s1 * (s1 / all), 0.f));
         }
-        sq = wave_sum(sq);
-        if (lane == 0) a.partial[size_t(blockIdx.x) * p.G + j] = make_float2(mean, sq);
     }
 }
 
@@ -238,17 +260,18 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs<T> a)
     const int lane = threadIdx.x & 63, width = p.C / p.G;
     for (int j = threadIdx.x >> 6; j < p.G; j += kThreads / 64) {  // the strips' sums of the element
         const float2 *part = a.partial + size_t(b) * p.strips * p.G + j;
+        const float mean0 = part[0].x;  // distances from one of the means: sums of them lose nothing
         int first;
-        float sum = 0.f;
-        for (int i = lane; i < p.strips; i += 64) sum = fmaf(float(rows_at(p, i, first)), part[size_t(i) * p.G].x, sum);
-        const float mean = wave_sum(sum) / float(p.L);
-        float sq = 0.f;
+        float s1 = 0.f, s2 = 0.f;
         for (int i = lane; i < p.strips; i += 64) {
             const float2 v = part[size_t(i) * p.G];
-            const float d = v.x - mean;
-            sq += fmaf(float(rows_at(p, i, first)) * float(width) * d, d, v.y);
+            const float d = v.x - mean0, n = float(rows_at(p, i, first)) * float(width);
+            s1 = fmaf(n, d, s1);
+            s2 += fmaf(n * d, d, v.y);
         }
-        const float rstd = 1.f / sqrtf(wave_sum(sq) / (float(p.L) * float(width)) + a.eps);
+        s1 = wave_sum(s1);
+        s2 = wave_sum(s2);
+        const float all = float(p.L) * float(width), mean = mean0 + s1 / all, rstd = 1.f / sqrtf(fmaxf(s2 - s1 * (s1 / all), 0.f) / all + a.eps);
         if (lane == 0) {
             stat[j] = make_float2(mean, rstd);
             if (strip == 0) *reinterpret_cast<float2 *>(a.stats + 2 * (size_t(b) * p.G + j)) = make_float2(mean, rstd);
@@ -263,13 +286,10 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs<T> a)
     for (int vec = p.row_groups > 1 ? int(threadIdx.x) - rg * p.vecs : int(threadIdx.x); vec < p.vecs; vec += kThreads) {
         const int n = rows_of_group(rows, rg, p.row_groups);
         Values<T> scale = vector_or(a.weight, vec * V, 1.f), bi = vector_or(a.bias, vec * V, 0.f);
-        float mean[V];
+        float mean[V], rstd[V];
+        by_group<T>(stat, vec * V, width, mean, rstd);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float2 v = stat[(vec * V + e) / width];
-            mean[e] = v.x;
-            scale.v[e] *= v.y;
-        }
+        for (int e = 0; e < V; ++e) scale.v[e] *= rstd[e];
         const size_t from = at + size_t(rg) * p.C + vec * V, step = size_t(p.row_groups) * p.C;
 #pragma unroll 4
         for (int i = 0; i < n; ++i) {
@@ -294,11 +314,10 @@ __device__ __forceinline__ Channels<T> channels_at(const NormArgs<T> &a, unsigne
     const Values<T> w = vector_or(a.weight, c, 1.f), bi = vector_or(a.bias, c, 0.f);
     const int width = a.p.C / a.p.G;
     Channels<T> ch;
+    const float2 *stats = reinterpret_cast<const float2 *>(a.in_stats) + size_t(b) * a.p.G;
+    by_group<T>(stats, c, width, ch.mean, ch.rstd);
 #pragma unroll
     for (int e = 0; e < kVec<T>; ++e) {
-        const float2 v = *reinterpret_cast<const float2 *>(a.in_stats + 2 * (size_t(b) * a.p.G + (c + e) / width));
-        ch.mean[e] = v.x;
-        ch.rstd[e] = v.y;
         ch.w[e] = w.v[e];
         ch.b[e] = bi.v[e];
     }
@@ -359,30 +378,34 @@ __global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormArgs<T> a)
     }
 }
 
-// The first workgroups join the strips' channel sums (64 channels each), the others write dx
+// The first workgroups join the strips' channel sums (kJoined channels each: few, for their chain of additions is what a launch of long strips
+// waits for), the others write dx
+constexpr int kJoined = 16;
 template <typename T, bool kSilu>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormArgs<T> a, unsigned joins)
 {
     constexpr int V = kVec<T>;
-    extern __shared__ __align__(16) float2 stat[];  // [G] m1, m2; or [4][64]
+    extern __shared__ __align__(16) float2 stat[];  // [G] m1, m2; or [kThreads]
     const Plan &p = a.p;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     if (blockIdx.x < joins) {
-        const int c = int(blockIdx.x) * 64 + lane;
+        const int c = int(blockIdx.x) * kJoined + int(threadIdx.x) % kJoined, row = int(threadIdx.x) / kJoined;
         float s1 = 0.f, s2 = 0.f;
         if (c < p.C)
 #pragma unroll 8
-            for (int i = w; i < p.B * p.strips; i += kThreads / 64) {
+            for (int i = row; i < p.B * p.strips; i += kThreads / kJoined) {
                 const float2 v = a.channel[size_t(i) * p.C + c];
                 s1 += v.x;
                 s2 += v.y;
             }
-        stat[w * 64 + lane] = make_float2(s1, s2);
+        stat[threadIdx.x] = make_float2(s1, s2);
         __syncthreads();
-        if (w == 0 && c < p.C) {
-            const float2 u = stat[lane], v = stat[64 + lane], x = stat[128 + lane], y = stat[192 + lane];
-            io<T>::store(a.d_bias + c, (u.x + v.x) + (x.x + y.x));
-            io<T>::store(a.d_weight + c, (u.y + v.y) + (x.y + y.y));
+        if (threadIdx.x < kJoined && c < p.C) {
+            s1 = s2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < kThreads / kJoined; ++i) s1 += stat[i * kJoined + threadIdx.x].x, s2 += stat[i * kJoined + threadIdx.x].y;
+            io<T>::store(a.d_bias + c, s1);
+            io<T>::store(a.d_weight + c, s2);
         }
         return;
     }
@@ -406,9 +429,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormArgs<T> a, unsi
     for (int vec = p.row_groups > 1 ? int(threadIdx.x) - rg * p.vecs : int(threadIdx.x); vec < p.vecs; vec += kThreads) {
         const int n = rows_of_group(rows, rg, p.row_groups);
         const Channels<T> ch = channels_at(a, b, vec * V);
-        float2 m[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) m[e] = stat[(vec * V + e) / width];
+        float m1[V], m2[V];
+        by_group<T>(stat, vec * V, width, m1, m2);
         const size_t from = at + size_t(rg) * p.C + vec * V, step = size_t(p.row_groups) * p.C;
 #pragma unroll 4
         for (int i = 0; i < n; ++i) {
@@ -418,7 +440,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormArgs<T> a, unsi
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float xn = (x.v[e] - ch.mean[e]) * ch.rstd[e], da = d.v[e] * act_slope<kSilu>(fmaf(xn, ch.w[e], ch.b[e]));
-                d.v[e] = ch.rstd[e] * (fmaf(da, ch.w[e], -m[e].x) - xn * m[e].y);
+                d.v[e] = ch.rstd[e] * (fmaf(da, ch.w[e], -m1[e]) - xn * m2[e]);
             }
             store(a.out + from + i * step, d);
         }
@@ -479,7 +501,7 @@ hipError_t backward(const NormArgs<T> &a, hipStream_t stream)
 {
     const Plan &p = a.p;
     const LaunchTimer timer(kKernelGroupNormBackward, stream);
-    const unsigned grid = unsigned(p.B) * unsigned(p.strips), joins = a.d_weight ? unsigned(p.C + 63) / 64 : 0;
+    const unsigned grid = unsigned(p.B) * unsigned(p.strips), joins = a.d_weight ? unsigned(p.C + kJoined - 1) / kJoined : 0;
     const size_t stat = size_t(p.G > 256 ? p.G : 256) * sizeof(float2);
     norm_sums_kernel<T, kSilu><<<grid, kThreads, size_t(p.row_groups) * p.C * sizeof(float2), stream>>>(a);
     norm_grad_kernel<T, kSilu><<<grid + joins, kThreads, stat, stream>>>(a, joins);
