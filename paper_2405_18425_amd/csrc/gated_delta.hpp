@@ -316,6 +316,8 @@ __device__ __forceinline__ unsigned row_offset(unsigned pitch, int token, int st
 // closed gate keeps its own decays.
 constexpr float kGateFloor = -10000.f;
 
+constexpr float kLeastStrength = 1e-20f;
+
 // Workspace of one chunk of one head, written by gd_prepare: c, beta, d and for the gradient 1 / beta (64 floats each), then fragments
 template <typename T, int N, bool kBwd>
 struct ChunkWs {

@@ -296,7 +296,7 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
                 const int item = 64 * i + lane, t = item >> 1;
                 tile_row<kC>(x, behind + Tile<DK>::bytes, t, item & 1);
                 float y[8];
-                const bool written = fabsf(done[i]) < 0.99e20f;  // beta is not the stand-in for zero
+                const bool written = fabsf(done[i]) < 0.99f / kLeastStrength;  // beta is not the stand-in for zero
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     y[j] = written ? x[j] : 0.f;
@@ -416,7 +416,7 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
     const int blocks = value_blocks(s.dv);
     const size_t state_bytes = emitted_bytes<T>(kCt, s.dv), token_bytes = emitted_bytes<T>(4, s.dv);
 
-    Gates<T, true> gates;
+    Gates<T, false> gates;
     In fo[kVs];
     Mid fr[kVs], fe[kVs], fs[kOwn], fd[kOwn];
     auto request_gates = [&](int h) __attribute__((always_inline)) { gates.request(a.g, a.beta, s, b, h, chunk, lane); };

@@ -340,7 +340,11 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            e[m] *= scalars(scal, kBeta, m, g);  // u
+            f32x4 beta = scalars(scal, kBeta, m, g);
+            if constexpr (kBwd)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) beta[i] = fabsf(beta[i]) <= kLeastStrength ? 0.f : beta[i];
+            e[m] *= beta;  // u
             if constexpr (!kBwd) *reinterpret_cast<f32x4 *>(hand + Hand::u + 1024 * m + 16 * lane) = e[m];
             e[m] *= scalars(scal, kD0, m, g);
         }

@@ -28,9 +28,9 @@ __device__ __forceinline__ void mma16(f32x4 &acc, const float *x, const float *y
     for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], y_col[(4 * g + i) * kPitch], acc, 0, 0, 0);
 }
 
-// beta as the gradient takes it: of a beta that is (next to) zero it needs w / beta, the gradient of u, which stays exact however small
-// beta is as long as it is not zero
-__device__ __forceinline__ float beta_divisor(float b) { return fabsf(b) < 1e-20f ? copysignf(1e-20f, b) : b; }
+// beta as the adjoints' chain takes it: of a beta that is (next to) zero it needs w / beta, the gradient of u, which stays exact however small
+// beta is as long as it is not zero.  Everything else takes beta as it is.
+__device__ __forceinline__ float beta_divisor(float b) { return fabsf(b) < kLeastStrength ? copysignf(kLeastStrength, b) : b; }
 
 // inclusive sums over the 64 lanes
 __device__ __forceinline__ double wave_prefix(double x, int lane)
