@@ -8,6 +8,7 @@ tensor is not on the GPU, the call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -460,6 +461,17 @@ def gated_bigla_fwd(x, w1, w2, q, k, v, bias=None, tau: float = 16.0, layout="bh
     return out, g_fwd, g_bwd
 
 
+def _as(t, name, shape, like, dtype, device: int):
+    """_dev(t, name, shape, like) where like has that dtype and device index: a small call is bound by what the host does for it,
+    and four comparisons take a third of what _dev takes."""
+    try:
+        if t.shape == shape and t.dtype is dtype and t.get_device() == device and t.is_contiguous():
+            return t
+    except AttributeError:
+        pass
+    return _dev(t, name, shape, like)
+
+
 def _fp32(t, name, shape, like):
     """An fp32 tensor (a state, statistics) beside tensors of either dtype."""
     t = _dev(t, name, shape)
@@ -468,26 +480,37 @@ def _fp32(t, name, shape, like):
     return t
 
 
+@functools.lru_cache(maxsize=256)
+def _bytes(query: str, *sizes) -> int:
+    """Workspace of a problem: a function of its sizes alone."""
+    return int(getattr(lib(), query)(*sizes))
+
+
+def _here(device):
+    """_on_device for a tensor's device index."""
+    return _SAME_DEVICE if torch._C._cuda_getDevice() == device else torch.cuda.device(device)
+
+
 def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
 def _workspace(workspace, need: int, device):
     """(workspace, bytes): the caller's, or one allocated with torch where some is needed."""
-    if workspace is None and need > 0:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    if workspace is not None:
-        workspace = _dev(workspace, "workspace")
-        if workspace.device != device:
-            raise VigError(VIG_ERR_DTYPE, "workspace must be on the device of the other tensors")
-    return workspace, workspace.numel() * workspace.element_size() if workspace is not None else 0
+    if workspace is None:
+        return (torch.empty(need, dtype=torch.uint8, device=device), need) if need > 0 else (None, 0)
+    workspace = _dev(workspace, "workspace")
+    if workspace.device != device:
+        raise VigError(VIG_ERR_DTYPE, "workspace must be on the device of the other tensors")
+    return workspace, workspace.numel() * workspace.element_size()
 
 
 def _delta_args(q, k, v, g, beta, layout, direction):
     lay = _layout_code(layout)
     if direction not in SCANS:
         raise VigError(VIG_ERR_UNSUPPORTED, f"direction must be one of {sorted(SCANS)}")
-    q, v = _dev(q, "q"), _dev(v, "v")
+    q = _dev(q, "q")
+    v = _dev(v, "v", like=q)
     if q.dim() != 4 or v.dim() != 4:
         raise VigError(VIG_ERR_SHAPE, "q and v must be 4-dimensional")
     if lay == VIG_LAYOUT_BHLD:
@@ -496,10 +519,12 @@ def _delta_args(q, k, v, g, beta, layout, direction):
         (B, L, Hk, dk), H = q.shape, v.shape[2]
     dv = v.shape[3]
     heads = (B, H, L) if lay == VIG_LAYOUT_BHLD else (B, L, H)
-    _dev(k, "k", q.shape, q)
-    _dev(v, "v", heads + (dv,), q)
-    _dev(g, "g", heads, q)
-    _dev(beta, "beta", heads, q)
+    dtype, device = q.dtype, q.get_device()
+    if v.shape != heads + (dv,):
+        raise VigError(VIG_ERR_SHAPE, "v must have the batch and length of q")
+    _as(k, "k", q.shape, q, dtype, device)
+    _as(g, "g", heads, q, dtype, device)
+    _as(beta, "beta", heads, q, dtype, device)
     return (B, H, Hk, L, dk, dv, _dtype_code(q)), lay, SCANS[direction]
 
 
@@ -522,14 +547,14 @@ def gated_delta_fwd(q, k, v, g, beta, initial_state=None, return_final_state=Fal
         _fp32(initial_state, "initial_state", (B, H, dk, dv), q)
     if final_state is None and return_final_state:
         final_state = torch.empty((B, H, dk, dv), dtype=torch.float32, device=q.device)
-    if final_state is not None:
+    elif final_state is not None:
         _fp32(final_state, "final_state", (B, H, dk, dv), q)
     out = torch.empty_like(v) if out is None else _dev(out, "out", v.shape, q)
-    workspace, ws_bytes = _workspace(workspace, gated_delta_workspace_bytes(*sizes), q.device)
-    with _on_device(q.device):
+    workspace, ws_bytes = _workspace(workspace, _bytes("gated_delta_workspace_bytes", *sizes), q.device)
+    with _here(q.get_device()):
         st = lib().gated_delta_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(),
                                    _ptr(initial_state), out.data_ptr(), _ptr(final_state), *sizes, lay, scan,
-                                   _ptr(workspace), ws_bytes, _stream_ptr(q.device))
+                                   _ptr(workspace), ws_bytes, torch._C._cuda_getCurrentRawStream(q.get_device()))
     _check(st, "gated_delta_fwd")
     return out if final_state is None else (out, final_state)
 
@@ -548,12 +573,12 @@ def gated_delta_bwd(q, k, v, g, beta, d_out, initial_state=None, d_final_state=N
     if d_final_state is not None:
         _fp32(d_final_state, "d_final_state", (B, H, dk, dv), q)
     grads = tuple(torch.empty_like(t) for t in (q, k, v, g, beta))
-    workspace, ws_bytes = _workspace(workspace, int(lib().gated_delta_bwd_workspace_bytes(*sizes)), q.device)
-    with _on_device(q.device):
+    workspace, ws_bytes = _workspace(workspace, _bytes("gated_delta_bwd_workspace_bytes", *sizes), q.device)
+    with _here(q.get_device()):
         st = lib().gated_delta_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(),
                                    _ptr(initial_state), d_out.data_ptr(), _ptr(d_final_state),
                                    *(t.data_ptr() for t in grads), _ptr(d_initial), *sizes, lay, scan, _ptr(workspace),
-                                   ws_bytes, _stream_ptr(q.device))
+                                   ws_bytes, torch._C._cuda_getCurrentRawStream(q.get_device()))
     _check(st, "gated_delta_bwd")
     return grads if d_initial is None else grads + (d_initial,)
 
@@ -564,25 +589,28 @@ def gated_delta_step(q, k, v, g, beta, state, slots=None, out=None):
     q, k: [B,Hk,dk]; v: [B,H,dv]; g, beta: [B,H]; slots: int32 [B], the state of each sequence (distinct; one outside
     [0, n_slots) marks a padded row, whose output is zero), or None (sequence b has state b) -> out [B,H,dv].
     """
-    q, v, state = _dev(q, "q"), _dev(v, "v"), _dev(state, "state")
+    q, state = _dev(q, "q"), _dev(state, "state")
+    v = _dev(v, "v", like=q)
     if q.dim() != 3 or v.dim() != 3 or state.dim() != 4:
         raise VigError(VIG_ERR_SHAPE, "q and v must be 3-dimensional, state 4-dimensional")
-    (B, Hk, dk), (_, H, dv) = q.shape, v.shape
-    _dev(k, "k", q.shape, q)
-    _dev(v, "v", (B, H, dv), q)
-    _dev(g, "g", (B, H), q)
-    _dev(beta, "beta", (B, H), q)
-    n_slots = state.shape[0]
-    _fp32(state, "state", (n_slots, H, dk, dv), q)
+    (B, Hk, dk), (_, H, dv), n_slots = q.shape, v.shape, state.shape[0]
+    dtype, device = q.dtype, q.get_device()
+    if v.shape[0] != B:
+        raise VigError(VIG_ERR_SHAPE, "v must have the leading dimension of q")
+    _as(k, "k", q.shape, q, dtype, device)
+    _as(g, "g", (B, H), q, dtype, device)
+    _as(beta, "beta", (B, H), q, dtype, device)
+    if state.dtype is not torch.float32 or state.get_device() != device or state.shape != (n_slots, H, dk, dv):
+        _fp32(state, "state", (n_slots, H, dk, dv), q)
     if slots is not None:
         _dev(slots, "slots", (B,))
         if slots.dtype != torch.int32 or slots.device != q.device:
             raise VigError(VIG_ERR_DTYPE, "slots must be int32, on the device of the other tensors")
     out = torch.empty_like(v) if out is None else _dev(out, "out", v.shape, q)
-    with _on_device(q.device):
+    with _here(q.get_device()):
         st = lib().gated_delta_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(),
                                     state.data_ptr(), _ptr(slots), out.data_ptr(), B, H, Hk, dk, dv, n_slots,
-                                    _dtype_code(q), _stream_ptr(q.device))
+                                    _dtype_code(q), torch._C._cuda_getCurrentRawStream(q.get_device()))
     _check(st, "gated_delta_step")
     return out
 
@@ -599,8 +627,8 @@ def _norm_args(x, groups, weight, bias, act):
     if (weight is None) != (bias is None):
         raise VigError(VIG_ERR_NULL, "weight and bias come together")
     if weight is not None:
-        _dev(weight, "weight", (C,), x)
-        _dev(bias, "bias", (C,), x)
+        _as(weight, "weight", (C,), x, x.dtype, x.get_device())
+        _as(bias, "bias", (C,), x, x.dtype, x.get_device())
     return (B, x.numel() // (B * C), C, groups), _dtype_code(x), ACTS[act]
 
 
@@ -613,11 +641,12 @@ def group_norm_act_fwd(x, groups: int, weight=None, bias=None, eps: float = 1e-5
     out = torch.empty_like(x) if out is None else _dev(out, "out", x.shape, x)
     if stats is None:
         stats = torch.empty((sizes[0], max(groups, 0), 2), dtype=torch.float32, device=x.device)
-    _fp32(stats, "stats", (sizes[0], groups, 2), x)
-    workspace, ws_bytes = _workspace(workspace, int(lib().group_norm_workspace_bytes(*sizes, code)), x.device)
-    with _on_device(x.device):
+    else:
+        _fp32(stats, "stats", (sizes[0], groups, 2), x)
+    workspace, ws_bytes = _workspace(workspace, _bytes("group_norm_workspace_bytes", *sizes, code), x.device)
+    with _here(x.get_device()):
         st = lib().group_norm_act_fwd(x.data_ptr(), _ptr(weight), _ptr(bias), out.data_ptr(), stats.data_ptr(), *sizes,
-                                      float(eps), act_code, code, _ptr(workspace), ws_bytes, _stream_ptr(x.device))
+                                      float(eps), act_code, code, _ptr(workspace), ws_bytes, torch._C._cuda_getCurrentRawStream(x.get_device()))
     _check(st, "group_norm_act_fwd")
     return out, stats
 
@@ -626,15 +655,15 @@ def group_norm_act_bwd(x, d_out, stats, groups: int, weight=None, bias=None, act
     """Gradient of group_norm_act_fwd: (dx, d_weight, d_bias) for the output gradient d_out and the forward's stats
     (d_weight and d_bias are None without a weight)."""
     sizes, code, act_code = _norm_args(x, groups, weight, bias, act)
-    _dev(d_out, "d_out", x.shape, x)
+    _as(d_out, "d_out", x.shape, x, x.dtype, x.get_device())
     _fp32(stats, "stats", (sizes[0], groups, 2), x)
     dx = torch.empty_like(x)
     dw, db = (torch.empty_like(weight), torch.empty_like(bias)) if weight is not None else (None, None)
-    workspace, ws_bytes = _workspace(workspace, int(lib().group_norm_bwd_workspace_bytes(*sizes, code)), x.device)
-    with _on_device(x.device):
+    workspace, ws_bytes = _workspace(workspace, _bytes("group_norm_bwd_workspace_bytes", *sizes, code), x.device)
+    with _here(x.get_device()):
         st = lib().group_norm_act_bwd(x.data_ptr(), _ptr(weight), _ptr(bias), stats.data_ptr(), d_out.data_ptr(),
                                       dx.data_ptr(), _ptr(dw), _ptr(db), *sizes, act_code, code, _ptr(workspace), ws_bytes,
-                                      _stream_ptr(x.device))
+                                      torch._C._cuda_getCurrentRawStream(x.get_device()))
     _check(st, "group_norm_act_bwd")
     return dx, dw, db
 
