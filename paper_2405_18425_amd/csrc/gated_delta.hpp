@@ -57,33 +57,69 @@ struct operands<float, N> {
     using Mid = Full;
 };
 
-__device__ __forceinline__ void mma(f32x4 &c, const Whole &a, const Whole &b) { c = mfma(a.v, b.v, c); }
+// A product of fragments is a sum of matrix instructions, term by term, the smallest first; terms below the last part's place are left out (a state's
+// extra part serves products with two as well).
+__device__ __forceinline__ constexpr int terms(const Whole &, const Whole &) { return 1; }
+__device__ __forceinline__ void term(f32x4 &c, const Whole &a, const Whole &b, int) { c = mfma(a.v, b.v, c); }
 template <int N>
-__device__ __forceinline__ void mma(f32x4 &c, const Whole &a, const Parts<N> &b)
+__device__ __forceinline__ constexpr int terms(const Whole &, const Parts<N> &)
 {
-#pragma unroll
-    for (int i = N - 1; i >= 0; --i) c = mfma(a.v, b.p[i], c);
+    return N;
 }
 template <int N>
-__device__ __forceinline__ void mma(f32x4 &c, const Parts<N> &a, const Whole &b)
+__device__ __forceinline__ void term(f32x4 &c, const Whole &a, const Parts<N> &b, int t)
 {
-#pragma unroll
-    for (int i = N - 1; i >= 0; --i) c = mfma(a.p[i], b.v, c);
+    c = mfma(a.v, b.p[N - 1 - t], c);
 }
-// products of parts below the last one's place are left out; a state's extra part serves products with two as well
+template <int N>
+__device__ __forceinline__ constexpr int terms(const Parts<N> &, const Whole &)
+{
+    return N;
+}
+template <int N>
+__device__ __forceinline__ void term(f32x4 &c, const Parts<N> &a, const Whole &b, int t)
+{
+    c = mfma(a.p[N - 1 - t], b.v, c);
+}
 template <int N, int M>
-__device__ __forceinline__ void mma(f32x4 &c, const Parts<N> &a, const Parts<M> &b)
+__device__ __forceinline__ constexpr int terms(const Parts<N> &, const Parts<M> &)
 {
     constexpr int kMost = N < M ? N : M;
-#pragma unroll
-    for (int s = kMost - 1; s >= 0; --s)
-#pragma unroll
-        for (int i = 0; i <= s; ++i) c = mfma(a.p[i], b.p[s - i], c);
+    return kMost * (kMost + 1) / 2;
 }
-__device__ __forceinline__ void mma(f32x4 &c, const Full &a, const Full &b)
+template <int N, int M>
+__device__ __forceinline__ void term(f32x4 &c, const Parts<N> &a, const Parts<M> &b, int t)
+{
+    static_assert(N <= 3 || M <= 3, "");
+    const int left = terms(a, b) - t, s = left > 3 ? 2 : left > 1 ? 1 : 0;  // parts whose places add up to s
+    const int i = (s + 1) * (s + 2) / 2 - left;
+    c = mfma(a.p[i], b.p[s - i], c);
+}
+__device__ __forceinline__ constexpr int terms(const Full &, const Full &) { return 8; }
+__device__ __forceinline__ void term(f32x4 &c, const Full &a, const Full &b, int t)
+{
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[t], b.v[t], c, 0, 0, 0);
+}
+template <typename A, typename B>
+__device__ __forceinline__ void mma(f32x4 &c, const A &a, const B &b)
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+    for (int t = 0; t < terms(a, b); ++t) term(c, a, b, t);
+}
+// acc[m] += a(m) b for m of [lo, hi): a term of every tile before the next one's, since an instruction waits for the one before it in its accumulator.
+// (32-bit instructions take as long as that wait; a tile at a time they begin before all of a has come.)
+template <typename A, typename B>
+__device__ __forceinline__ void mma_tiles(f32x4 *acc, int lo, int hi, const A &a, const B &b)
+{
+    if constexpr (std::is_same<B, Full>::value) {
+#pragma unroll
+        for (int m = lo; m < hi; ++m) mma(acc[m], a(m), b);
+        return;
+    }
+#pragma unroll
+    for (int t = 0; t < terms(a(0), b); ++t)
+#pragma unroll
+        for (int m = lo; m < hi; ++m) term(acc[m], a(m), b, t);
 }
 
 // eight 32-bit values as an operand
@@ -278,7 +314,8 @@ struct Walk {
     unsigned extent, last_extent;
     int chunk, move, last_chunk;
 
-    __device__ __forceinline__ Rsrc here() const { return slab_resource(p, chunk == last_chunk ? last_extent : extent); }
+    // `there`: or nothing, what is read is zero and what is written goes nowhere
+    __device__ __forceinline__ Rsrc here(bool there = true) const { return slab_resource(p, !there ? 0u : chunk == last_chunk ? last_extent : extent); }
     __device__ __forceinline__ void next() { p += step, chunk += move; }
 };
 // `first`: the chunk it starts with, `move`: +1 or -1
@@ -318,14 +355,15 @@ constexpr float kGateFloor = -10000.f;
 
 constexpr float kLeastStrength = 1e-20f;
 
-// Workspace of one chunk of one head, written by gd_prepare: c, beta, d and for the gradient 1 / beta (64 floats each), then fragments
+// Workspace of one chunk of one head, written by gd_prepare: c, d . beta and for the gradient d . beta and 1 / beta with the stand-in for a beta of zero
+// (64 floats each), then fragments
 template <typename T, int N, bool kBwd>
 struct ChunkWs {
     using Mid = typename operands<T, N>::Mid;
     using Mid2 = typename operands<T, 2>::Mid;
     static constexpr size_t scalars = 0;
     static constexpr size_t inverse = 1024;                                          // That, or its transpose too
-    static constexpr size_t scores = inverse + kTriBlocks * frag_bytes<Mid> * (kBwd ? 2 : 1);  // P, or P^T
+    static constexpr size_t scores = inverse + kTriBlocks * frag_bytes<Mid> * (kBwd ? 2 : 1);  // P diag(beta), or its transpose
     static constexpr size_t bytes = scores + kTriBlocks * (kBwd ? frag_bytes<Mid> : frag_bytes<Mid2>);
 };
 // ... and of one chunk of one key head: K^T, and for the gradient Q^T

@@ -40,10 +40,10 @@ struct AdjointArgs {
 };
 
 // The chain of the adjoints for 16 value columns, last chunk first, the counterpart of gd::states: one wave holds D and takes the three products
-// that depend on it; a second one makes what does not, P^T dO and Q^T (c . dO), a chunk ahead, and takes D, w and r away, a chunk behind.
+// that depend on it; a second one makes what does not, (P diag(beta))^T dO and Q^T (c . dO), a chunk ahead, and takes D, w and r away, a chunk behind.
 template <int DK>
 struct AdjointLds {
-    static constexpr int ahead = 4096 + DK * 64;                     // P^T dO, Q^T (c . dO): accumulators, 16 bytes a lane
+    static constexpr int ahead = 4096 + DK * 64;                     // (P diag(beta))^T dO, Q^T (c . dO): accumulators, 16 bytes a lane
     static constexpr int behind = Tile<DK>::bytes + Tile<kC>::bytes;  // D, w
     static constexpr int bytes = 2 * (ahead + behind);
 };
@@ -131,25 +131,22 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
         for (int m = 0; m < 4; ++m) u[m] = zero;
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks)
-#pragma unroll
-            for (int m = 0; m < 4; ++m) mma(u[m], fk[m][ks], fd[ks]);
+            mma_tiles(u, 0, 4, [&](int m) -> const In & { return fk[m][ks]; }, fd[ks]);
         requests_stay();
         load_keys();
         requests_stay();
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const f32x4 d = scalars(scal, kD0, m, g), pd = *reinterpret_cast<const f32x4 *>(ahead + 1024 * m + 16 * lane);
+            const f32x4 d = scalars(scal, kRead, m, g), pd = *reinterpret_cast<const f32x4 *>(ahead + 1024 * m + 16 * lane);
 #pragma unroll
             for (int i = 0; i < 4; ++i) u[m][i] = fmaf(d[i], u[m][i], pd[i]);
-            u[m] *= scalars(scal, kBeta, m, g);
         }
         const Mid fu[2] = {from<Mid>(u[0], u[1]), from<Mid>(u[2], u[3])};
 #pragma unroll
         for (int m = 0; m < 4; ++m) u[m] = zero;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int m = 0; m <= 2 * ks + 1; ++m) mma(u[m], ft[upper_block(m, ks)], fu[ks]);
+            mma_tiles(u, 0, 2 * ks + 2, [&](int m) -> const Mid & { return ft[upper_block(m, ks)]; }, fu[ks]);
         requests_stay();
         load_inverse();
         requests_stay();
@@ -168,8 +165,7 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
         }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int ct = 0; ct < kCt; ++ct) mma(D[ct], fkt[ct][ks], fw[ks]);
+            mma_tiles(D, 0, kCt, [&](int ct) -> const In & { return fkt[ct][ks]; }, fw[ks]);
         requests_stay();
         load_transposed();
         requests_stay();
@@ -185,7 +181,7 @@ __device__ __forceinline__ void adjoint_chain(const AdjointArgs<T> &a, const Col
 }
 
 template <typename T, int DK, int N>
-__device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Columns &at, unsigned char *own /* the wave's: scalars, then a strip */,
+__device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Columns &at, unsigned char *own /* the wave's: two chunks' scalars, then a strip */,
                                               unsigned char *lds)
 {
     using In = typename operands<T, N>::In;
@@ -205,115 +201,133 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
     const size_t state_bytes = emitted_bytes<T>(DK / 16, s.dv), token_bytes = emitted_bytes<T>(4, s.dv), units = size_t(at.slab) * s.chunks;
 
     const int first = chunk_at(s, s.chunks - 1), move = s.reverse ? 1 : -1;
-    Walk dor = walk_rows(a.d_out, s, at.b, at.h, s.H, s.dv, first, move), dvr = walk_rows(static_cast<const T *>(a.dv), s, at.b, at.h, s.H, s.dv, first, move),
-         ws = walk_blocks(a.ws + units * Ws::bytes, Ws::bytes, first, move), inv = ws,
+    // (what is taken away starts a chunk late)
+    Walk dor = walk_rows(a.d_out, s, at.b, at.h, s.H, s.dv, first, move),
+         dvr = walk_rows(static_cast<const T *>(a.dv), s, at.b, at.h, s.H, s.dv, first - move, move),
+         ws = walk_blocks(a.ws + units * Ws::bytes, Ws::bytes, first, move),
          kw = walk_blocks(a.key_ws + (size_t(at.b) * s.Hk + at.hk) * s.chunks * Kw::bytes, Kw::bytes, first, move),
-         to_d = walk_blocks(a.adjoints + units * state_bytes, state_bytes, first, move), to_r = walk_blocks(a.r + units * token_bytes, token_bytes, first, move);
+         to_d = walk_blocks(a.adjoints + units * state_bytes, state_bytes, first - move, move),
+         to_r = walk_blocks(a.r + units * token_bytes, token_bytes, first - move, move);
     In fqt[kCt][2];
     Mid fp[kTriBlocks];
     Strip<T> dout;
     u32x4 raw;
-    auto request = [&]() __attribute__((always_inline)) {
-        const Rsrc ws0 = ws.here(), kw0 = kw.here(), do0 = dor.here();
-        ws.next(), kw.next(), dor.next();
-        raw = request_scalars(ws0, lane);
+    int left = s.chunks;  // chunks from the one requested on
+    auto request_rows = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = dor.here();
+        raw = request_scalars(ws.here(), lane);
 #pragma unroll
-        for (int l = 0; l < Strip<T>::loads; ++l) dout.w[l] = load16(do0, value_at[l]);
-#pragma unroll
-        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid>(ws0, Ws::scores, i, lane);
-#pragma unroll
-        for (int ct = 0; ct < kCt; ++ct)
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) fqt[ct][ks] = get<In>(kw0, Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
+        for (int l = 0; l < Strip<T>::loads; ++l) dout.w[l] = load16(from0, value_at[l]);
     };
-    auto make_ahead = [&](unsigned char *to) __attribute__((always_inline)) {
+    auto request_scores = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = ws.here();
+#pragma unroll
+        for (int i = 0; i < kTriBlocks; ++i) fp[i] = get<Mid>(from0, Ws::scores, i, lane);
+    };
+    auto request_queries = [&]() __attribute__((always_inline)) {
+        const Rsrc from0 = kw.here();
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int ct = 0; ct < kCt; ++ct) fqt[ct][ks] = get<In>(from0, Kw::blocks * frag_bytes<In>, 2 * ct + ks, lane);
+    };
+    // a chunk's part without D, and the requests of the next one as registers become free (what is made ahead of the last step is never read)
+    auto make_ahead = [&](int step) __attribute__((always_inline)) {
+        unsigned char *to = lds + (step & 1) * Lds::ahead, *scal = own + (step & 1) * kScalarBytes, *strip = own + 2 * kScalarBytes;
+        if (--left > 0) ws.next(), kw.next(), dor.next();
         In fo[2];
         Mid fod[2];
-        strip_put(own + kScalarBytes, dout, lane);
-        share_scalars(own, raw, lane);
+        strip_put(strip, dout, lane);
+        share_scalars(scal, raw, lane);
+        requests_stay();
+        request_rows();
+        requests_stay();
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
             T x[8];
             float y[8];
-            strip_column(x, own + kScalarBytes, p, at.r, g);
-            const f32x4 c[2] = {scalars(own, kC0, 2 * p, g), scalars(own, kC0, 2 * p + 1, g)};
+            strip_column(x, strip, p, at.r, g);
+            const f32x4 c[2] = {scalars(scal, kC0, 2 * p, g), scalars(scal, kC0, 2 * p + 1, g)};
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = value(x[j]) * c[j >> 2][j & 3];
             gather(fo[p], x);
             make(fod[p], y);
         }
-        f32x4 pd[4], qd[kCt];
+        f32x4 w[4], qd[kCt];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) pd[m] = zero;
+        for (int m = 0; m < 4; ++m) w[m] = zero;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+            mma_tiles(w, 0, 2 * ks + 2, [&](int m) -> const Mid & { return fp[upper_block(m, ks)]; }, fo[ks]);
+        requests_stay();
+        request_scores();
+        requests_stay();
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) qd[ct] = zero;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
+        for (int ks = 0; ks < 2; ++ks)
+            mma_tiles(qd, 0, kCt, [&](int ct) -> const In & { return fqt[ct][ks]; }, fod[ks]);
+        requests_stay();
+        request_queries();
+        requests_stay();
 #pragma unroll
-            for (int m = 0; m <= 2 * ks + 1; ++m) mma(pd[m], fp[upper_block(m, ks)], fo[ks]);
-#pragma unroll
-            for (int ct = 0; ct < kCt; ++ct) mma(qd[ct], fqt[ct][ks], fod[ks]);
-        }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4 *>(to + 1024 * m + 16 * lane) = pd[m];
+        for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4 *>(to + 1024 * m + 16 * lane) = w[m];
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) *reinterpret_cast<f32x4 *>(to + 4096 + 1024 * ct + 16 * lane) = qd[ct];
     };
-    request();
-    make_ahead(lds + ((s.chunks - 1) & 1) * Lds::ahead);
-    if (s.chunks > 1) request();
-    float inverse[2] = {0.f, 0.f};
-    for (int step = s.chunks - 1; step >= -1; --step) {
+    // takes chunk `step` away; one that is not there goes nowhere
+    auto take = [&](int step) __attribute__((always_inline)) {
+        const unsigned char *behind = lds + 2 * Lds::ahead + (step & 1) * Lds::behind, *scal = own + (step & 1) * kScalarBytes;
+        const bool there = step < s.chunks;
+        const Rsrc to = to_d.here(there), tr = to_r.here(there), dv0 = dvr.here(there);
+        to_d.next(), to_r.next(), dvr.next();
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < DK / 32; ++i) {
+            const int item = 64 * i + lane;
+            tile_row<DK>(x, behind, item >> 1, item & 1);
+            emit<Mid2>(to, unpaired(item >> 1), part, item & 1, s.dv, x);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int item = 64 * i + lane, t = item >> 1;
+            tile_row<kC>(x, behind + Tile<DK>::bytes, t, item & 1);
+            const float inverse = *reinterpret_cast<const float *>(scal + kInverseBeta + 4 * t);
+            const bool written = fabsf(inverse) < 0.99f / kLeastStrength;  // beta is not the stand-in for zero
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                y[j] = written ? x[j] : 0.f;
+                x[j] *= inverse;
+            }
+            store_row(dv0, unsigned(token_at(s, t)) * value_pitch + unsigned(16 * part + 8 * (item & 1)) * unsigned(sizeof(T)), y, T{});
+            emit<Mid2>(tr, natural(t), part, item & 1, s.dv, x);
+        }
+    };
+    // (no branches around requests and stores: a wait counts what was asked for behind what it is for, and where paths with different counts
+    // meet, that is everything)
+    request_rows();
+    requests_stay();
+    request_scores();
+    requests_stay();
+    request_queries();
+    requests_stay();
+    make_ahead(s.chunks - 1);
+    for (int step = s.chunks - 1; step >= 0; --step) {
         __syncthreads();
-        const float done[2] = {inverse[0], inverse[1]};  // 1 / beta of the rows that this lane takes away
-        if (step >= 0) {
-            const Rsrc ws0 = inv.here();
-            inv.next();
-#pragma unroll
-            for (int i = 0; i < 2; ++i) inverse[i] = load4(ws0, 4u * unsigned((64 * i + lane) >> 1), kInverseBeta);
-        }
-        if (step > 0) {
-            make_ahead(lds + ((step - 1) & 1) * Lds::ahead);
-            if (step > 1) {
-                requests_stay();
-                request();
-                requests_stay();
-            }
-        }
-        if (step + 1 < s.chunks) {
-            const unsigned char *behind = lds + 2 * Lds::ahead + ((step + 1) & 1) * Lds::behind;
-            const Rsrc to = to_d.here(), tr = to_r.here(), dv0 = dvr.here();
-            to_d.next(), to_r.next(), dvr.next();
-            float x[8];
-#pragma unroll
-            for (int i = 0; i < DK / 32; ++i) {
-                const int item = 64 * i + lane;
-                tile_row<DK>(x, behind, item >> 1, item & 1);
-                emit<Mid2>(to, unpaired(item >> 1), part, item & 1, s.dv, x);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int item = 64 * i + lane, t = item >> 1;
-                tile_row<kC>(x, behind + Tile<DK>::bytes, t, item & 1);
-                float y[8];
-                const bool written = fabsf(done[i]) < 0.99f / kLeastStrength;  // beta is not the stand-in for zero
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    y[j] = written ? x[j] : 0.f;
-                    x[j] *= done[i];
-                }
-                store_row(dv0, unsigned(token_at(s, t)) * value_pitch + unsigned(16 * part + 8 * (item & 1)) * unsigned(sizeof(T)), y, T{});
-                emit<Mid2>(tr, natural(t), part, item & 1, s.dv, x);
-            }
-        }
+        take(step + 1);
+        requests_stay();
+        make_ahead(step - 1);
     }
+    __syncthreads();
+    take(0);
 }
 
 // Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'
 template <typename T, int DK, int N>
 __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(chain_waves<T, DK>, chain_waves<T, DK>))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
 {
-    __shared__ __align__(16) unsigned char lds[AdjointLds<DK>::bytes], scal[kScalarBytes + Strip<T>::bytes], own[kScalarBytes + Strip<T>::bytes];
+    __shared__ __align__(16) unsigned char lds[AdjointLds<DK>::bytes], scal[kScalarBytes + Strip<T>::bytes], own[2 * kScalarBytes + Strip<T>::bytes];
     Columns at;
     if (!columns_of(a.s, at)) return;
     if (blockIdx.y == 0) {
@@ -427,7 +441,7 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
                    Dr = whole(a.adjoints + value_unit * state_bytes);
 #pragma unroll
         for (int ks = 0; ks < kVs; ++ks) {
-            const unsigned nowhere = v0 + ks < blocks ? 0u : kNowhere;
+            const unsigned nowhere = 32 * (v0 + ks) + 8 * g < s.dv ? 0u : kNowhere;
             load_row(fo[ks], dor, row_offset<T>(value_pitch, token_at(s, 16 * w + r), v0 + ks, g, s.dv));
             fe[ks] = get_at<Mid>(er, nowhere, w * blocks + v0 + ks, lane);
             fr[ks] = get_at<Mid>(rr, nowhere, w * blocks + v0 + ks, lane);
@@ -435,7 +449,7 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
 #pragma unroll
         for (int o = 0; o < kOwn; ++o) {
             const int block = 4 * o + w, ct = block / kVs, ks = block % kVs;
-            const unsigned nowhere = block < kCt * kVs && v0 + ks < blocks ? 0u : kNowhere;
+            const unsigned nowhere = block < kCt * kVs && 32 * (v0 + ks) + 8 * g < s.dv ? 0u : kNowhere;
             fs[o] = get_at<Mid>(Sr, nowhere, ct * blocks + v0 + ks, lane);
             fd[o] = get_at<Mid>(Dr, nowhere, ct * blocks + v0 + ks, lane);
         }

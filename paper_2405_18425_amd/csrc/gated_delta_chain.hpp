@@ -54,7 +54,7 @@ __device__ __forceinline__ void share_scalars(unsigned char *lds, const u32x4 &x
     wave_fence();
 }
 // of the tokens that accumulators of tile m stand for
-enum Scalar { kC0 = 0, kBeta = 256, kD0 = 512, kInverseBeta = 768 };
+enum Scalar { kC0 = 0, kWritten = 256 /* d . beta */, kRead = 512, kInverseBeta = 768 };
 __device__ __forceinline__ f32x4 scalars(const unsigned char *lds, Scalar which, int m, int g)
 {
     return *reinterpret_cast<const f32x4 *>(lds + which + 128 * (m >> 1) + 16 * (m & 1) + 32 * g);
@@ -68,12 +68,12 @@ __device__ __forceinline__ unsigned state_offset(const Shape &s, int ct, int i, 
     return c < s.dk ? 4u * (unsigned(c) * unsigned(s.dv) + unsigned(col)) : kNowhere;
 }
 
-// What the chain of a chunk leaves for its outputs, in LDS: the state as fragments (two parts) and u as it is
+// What the chain of a chunk leaves for its outputs, in LDS: the state as fragments (two parts) and e as it is
 template <typename T, int DK>
 struct HandOver {
     using Mid2 = typename operands<T, 2>::Mid;
-    static constexpr int u = DK / 32 * int(frag_bytes<Mid2>);
-    static constexpr int bytes = u + 4096;
+    static constexpr int e = DK / 32 * int(frag_bytes<Mid2>);
+    static constexpr int bytes = e + 4096;
 };
 template <typename Frag>
 __device__ __forceinline__ void lds_put(unsigned char *lds, int block, int lane, const Frag &f)
@@ -182,7 +182,7 @@ struct Place {
 __device__ __forceinline__ Place natural(int row) { return {row >> 4, row & 15}; }
 __device__ __forceinline__ Place unpaired(int row) { return {2 * (row >> 5) + ((row >> 2) & 1), 4 * ((row >> 3) & 3) + (row & 3)}; }
 
-// eight columns of a row as a fragment's lane; where the head has 16 columns only, the other half of the fragment is zero
+// eight columns of a row as a fragment's lane (of a head whose last block has 16 columns, the other half is not written: who reads it leaves it out)
 template <typename Mid2>
 __device__ __forceinline__ void emit(Rsrc to, Place at, int part, int group, int dv, const float (&x)[8])
 {
@@ -193,10 +193,7 @@ __device__ __forceinline__ void emit(Rsrc to, Place at, int part, int group, int
     const unsigned block = unsigned(at.tile * value_blocks(dv) + (part >> 1)) * unsigned(frag_bytes<Mid2>);
     const unsigned off = block + 16u * unsigned(at.r + 16 * (2 * (part & 1) + group));
 #pragma unroll
-    for (int p = 0; p < planes<Mid2>; ++p) {
-        __builtin_amdgcn_raw_buffer_store_b128(w[p], to, off + 1024u * unsigned(p), 0, 0);
-        if (dv == 16) __builtin_amdgcn_raw_buffer_store_b128(u32x4{0, 0, 0, 0}, to, off + 512u + 1024u * unsigned(p), 0, 0);
-    }
+    for (int p = 0; p < planes<Mid2>; ++p) __builtin_amdgcn_raw_buffer_store_b128(w[p], to, off + 1024u * unsigned(p), 0, 0);
 }
 template <int kRows>
 __device__ __forceinline__ void tile_row(float (&x)[8], const unsigned char *lds, int row, int group)
@@ -308,8 +305,7 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
         for (int m = 0; m < 4; ++m) e[m] = zero;
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks)
-#pragma unroll
-            for (int m = 0; m < 4; ++m) mma(e[m], fk[m][ks], fs[ks]);
+            mma_tiles(e, 0, 4, [&](int m) -> const In & { return fk[m][ks]; }, fs[ks]);
         requests_stay();
         load_keys();
         requests_stay();
@@ -329,33 +325,25 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
         for (int m = 0; m < 4; ++m) e[m] = zero;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int m = 2 * ks; m < 4; ++m) mma(e[m], ft[lower_block(m, ks)], fe[ks]);
+            mma_tiles(e, 2 * ks, 4, [&](int m) -> const Mid & { return ft[lower_block(m, ks)]; }, fe[ks]);
         requests_stay();
         load_inverse();
         requests_stay();
-        if constexpr (kBwd) {
-#pragma unroll
-            for (int m = 0; m < 4; ++m) tile_put<kC>(hand + Tile<DK>::bytes, m, r, g, e[m]);
-        }
+        const float whole = whole_decay(scal);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            f32x4 beta = scalars(scal, kBeta, m, g);
             if constexpr (kBwd)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) beta[i] = fabsf(beta[i]) <= kLeastStrength ? 0.f : beta[i];
-            e[m] *= beta;  // u
-            if constexpr (!kBwd) *reinterpret_cast<f32x4 *>(hand + Hand::u + 1024 * m + 16 * lane) = e[m];
-            e[m] *= scalars(scal, kD0, m, g);
+                tile_put<kC>(hand + Tile<DK>::bytes, m, r, g, e[m]);
+            else
+                *reinterpret_cast<f32x4 *>(hand + Hand::e + 1024 * m + 16 * lane) = e[m];
+            e[m] *= scalars(scal, kWritten, m, g);
         }
-        const float whole = whole_decay(scal);
         const Mid fd[2] = {from<Mid>(e[0], e[1]), from<Mid>(e[2], e[3])};
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) S[ct] *= whole;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int ct = 0; ct < kCt; ++ct) mma(S[ct], fkt[ct][ks], fd[ks]);
+            mma_tiles(S, 0, kCt, [&](int ct) -> const In & { return fkt[ct][ks]; }, fd[ks]);
         requests_stay();
         load_transposed();
         requests_stay();
@@ -454,29 +442,27 @@ __device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at
         if (step + 1 < s.chunks) qr.next(), ws.next();
         const unsigned char *hand = lds + (step & 1) * Hand::bytes;
         share_scalars(own, raw, lane);
-        __syncthreads();  // the chain has left this chunk's state and u; it writes the other half until the next one
-        f32x4 o[4], u[4];
+        __syncthreads();  // the chain has left this chunk's state and e; it writes the other half until the next one
+        f32x4 o[4], e[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             o[m] = zero;
-            u[m] = *reinterpret_cast<const f32x4 *>(hand + Hand::u + 1024 * m + 16 * lane);
+            e[m] = *reinterpret_cast<const f32x4 *>(hand + Hand::e + 1024 * m + 16 * lane);
         }
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) {
             const Mid2 fs = lds_get<Mid2>(hand, ks, lane);
-#pragma unroll
-            for (int m = 0; m < 4; ++m) mma(o[m], fq[m][ks], fs);
+            mma_tiles(o, 0, 4, [&](int m) -> const In & { return fq[m][ks]; }, fs);
         }
         requests_stay();
         load_queries();
         requests_stay();
-        const Mid2 fu[2] = {from<Mid2>(u[0], u[1]), from<Mid2>(u[2], u[3])};
+        const Mid2 fe[2] = {from<Mid2>(e[0], e[1]), from<Mid2>(e[2], e[3])};
 #pragma unroll
         for (int m = 0; m < 4; ++m) o[m] *= scalars(own, kC0, m, g);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int m = 2 * ks; m < 4; ++m) mma(o[m], fp[lower_block(m, ks)], fu[ks]);
+            mma_tiles(o, 2 * ks, 4, [&](int m) -> const Mid2 & { return fp[lower_block(m, ks)]; }, fe[ks]);
         requests_stay();
         load_scores();
         requests_stay();

@@ -131,10 +131,13 @@ __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
         sum[w][lane] = p;
         bet[w][lane] = beta;
         if (w == 0) {
+            const float d = exp2_of(total - p);
             store4(ws, 4u * unsigned(lane), exp2_of(p));
-            store4(ws, 4u * unsigned(lane), beta, 4 * kC);
-            store4(ws, 4u * unsigned(lane), exp2_of(total - p), 8 * kC);
-            if constexpr (kBwd) store4(ws, 4u * unsigned(lane), 1.f / beta, 12 * kC);
+            store4(ws, 4u * unsigned(lane), d * value(gates.beta), 4 * kC);
+            if constexpr (kBwd) {
+                store4(ws, 4u * unsigned(lane), d * beta, 8 * kC);
+                store4(ws, 4u * unsigned(lane), 1.f / beta, 12 * kC);
+            }
         }
     }
 #pragma unroll
@@ -176,8 +179,8 @@ __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * w + 4 * g + i, c = 16 * n + r;
             // (factors of 0 and 1 rather than branches)
-            const float decay = exp2_of(c <= t ? sum[w][t] - sum[w][c] : 0.0);
-            inv[t * kPitch + c] = (c < t ? 1.f : 0.f) * decay * bet[w][c] * kk[n][i];
+            const float decay = exp2_of(c <= t ? sum[w][t] - sum[w][c] : 0.0) * bet[w][c];
+            inv[t * kPitch + c] = (c < t ? 1.f : 0.f) * decay * kk[n][i];
             sco[t * kPitch + c] = (c <= t ? 1.f : 0.f) * decay * qk[n][i];
         }
     __syncthreads();
