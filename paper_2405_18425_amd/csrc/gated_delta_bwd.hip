@@ -21,11 +21,13 @@ namespace {
 
 using namespace gd;
 
-__device__ __forceinline__ float wave_total(float x)
+// sums over the four rows of 16 lanes
+__device__ __forceinline__ float rows_total(float x)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-    return x;
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
 template <typename T>
@@ -455,6 +457,11 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
         }
     };
 
+    auto put_gates = [&]() __attribute__((always_inline)) {
+        sum[w][lane] = gates.sum();
+        bet[w][lane] = gates.strength();
+    };
+
     f32x4 dq[kCt], dk[kCt];
     In fq[kKs], fk[kKs], fkc[Kw::blocks / 2];
     {
@@ -471,6 +478,7 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
         request_slice(hk * share, 0);
         requests_stay();
     }
+    put_gates();
 #pragma unroll
     for (int ks = 0; ks < kKs; ++ks) lds_put(key_rows, w * kKs + ks, lane, fk[ks]);
 #pragma unroll
@@ -491,9 +499,8 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
             request_gates(h);
             request_slice(h, 0);
             requests_stay();
+            put_gates();
         }
-        sum[w][lane] = gates.sum(lane);
-        bet[w][lane] = gates.strength();
         float ds = 0.f;  // <D, S>
         for (int v0 = 0; v0 < (kOne ? 1 : blocks); v0 += kVs) {
             if (!kOne && v0 > 0) {
@@ -529,8 +536,8 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
             }
             __syncthreads();
         }
-        ds = wave_total(ds);
-        if (lane == 0) through[w] = ds;
+        ds = wave_prefix(ds);
+        if (lane == 63) through[w] = ds;
 
         // X, Y and the pairs' part of dg
         {  // r_t . e_t stands on the diagonal of y
@@ -539,6 +546,9 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
             store_element<T>(chunk_rows(a.dbeta, s, b, h, s.H, 1, chunk), (r >> 2) == g ? unsigned(token_at(s, 16 * w + r)) * pitch_of<T>(s, s.H, 1) : kNowhere, db);
         }
         float carry[4] = {0.f, 0.f, 0.f, 0.f};
+        In own[kKs];  // the wave's rows of k
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) own[ks] = lds_get<In>(key_rows, w * kKs + ks, lane);
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             float column = 0.f;
@@ -549,23 +559,22 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
             for (int ks = 0; ks < kKs; ++ks) {
                 const In f = lds_get<In>(key_rows, n * kKs + ks, lane);
                 mma(qk, fq[ks], f);
-                mma(kk, fk[ks], f);
+                mma(kk, own[ks], f);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int t = 16 * w + 4 * g + i;
                 // (factors of 0 and 1 rather than branches)
                 const float upto_t = c <= t ? 1.f : 0.f, before_t = c < t ? 1.f : 0.f;
-                const float decay = exp2_of(c <= t ? sum[w][t] - sum[w][c] : 0.0) * bet[w][c];
+                const float decay = decay_of(sum[w][t], sum[w][c], c <= t) * bet[w][c];
                 const float xi = upto_t * decay * x[n][i], yi = before_t * -decay * bet[w][t] * y[n][i];
                 X[t * kPitch + c] = xi;
                 Y[t * kPitch + c] = yi;
                 const float z = before_t * xi * qk[i] + yi * kk[i], upto = row_scan<0>(z);
                 column += upto_t * (upto - z + carry[i]);  // pairs (t, i < c)
-                carry[i] += __shfl(upto, lane | 15);
+                carry[i] += moved<0x15f, 0xf>(upto);  // row_newbcast:15
             }
-            column += __shfl_xor(column, 16);
-            column += __shfl_xor(column, 32);
+            column = rows_total(column);
             if (g == 0) pairs[w][c] = column;
         }
         f32x4 enter = zero, leave = zero;
@@ -621,15 +630,10 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
             }
         }
         if (w == 0) {
-            float after = enters[lane], before = leaves[lane];
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const float u = __shfl_down(after, d), v = __shfl_up(before, d);
-                after += lane + d < 64 ? u : 0.f;
-                before += lane >= d ? v : 0.f;
-            }
-            const float earlier = __shfl_up(before, 1);
-            before = lane > 0 ? earlier : 0.f;
+            const float suffix = wave_prefix(enters[kC - 1 - lane]), before = moved<0x138, 0xf>(wave_prefix(leaves[lane]));  // wave_shr:1
+            enters[kC - 1 - lane] = suffix;
+            wave_fence();
+            const float after = enters[lane];
             const float state = exp2_of(sum[w][kC - 1]) * ((through[0] + through[1]) + (through[2] + through[3]));
             const float dg = after + before + ((pairs[0][lane] + pairs[1][lane]) + (pairs[2][lane] + pairs[3][lane])) + state;
             store_element<T>(chunk_rows(a.dg, s, b, h, s.H, 1, chunk), unsigned(token_at(s, lane)) * pitch_of<T>(s, s.H, 1), dg);

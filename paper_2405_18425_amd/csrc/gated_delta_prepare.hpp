@@ -32,15 +32,34 @@ __device__ __forceinline__ void mma16(f32x4 &acc, const float *x, const float *y
 // beta is as long as it is not zero.  Everything else takes beta as it is.
 __device__ __forceinline__ float beta_divisor(float b) { return fabsf(b) < kLeastStrength ? copysignf(kLeastStrength, b) : b; }
 
-// inclusive sums over the 64 lanes
-__device__ __forceinline__ double wave_prefix(double x, int lane)
+// DPP: a lane's source in its row of 16 or the row before; lanes without one, and rows that are not in the mask, receive 0
+template <int CTRL, int kRows>
+__device__ __forceinline__ float moved(float x)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double y = __shfl_up(x, d);
-        x += lane >= d ? y : 0.0;
-    }
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, kRows, 0xf, false));
+}
+template <int CTRL, int kRows>
+__device__ __forceinline__ double moved(double x)
+{
+    const int2 w = __builtin_bit_cast(int2, x);
+    return __builtin_bit_cast(double, int2{__builtin_amdgcn_update_dpp(0, w.x, CTRL, kRows, 0xf, false), __builtin_amdgcn_update_dpp(0, w.y, CTRL, kRows, 0xf, false)});
+}
+// inclusive sums over the 64 lanes
+template <typename F>
+__device__ __forceinline__ F wave_prefix(F x)
+{
+    x += moved<0x111, 0xf>(x);  // row_shr:1
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x);  // row_bcast:15, rows 1 and 3
+    x += moved<0x143, 0xc>(x);  // row_bcast:31, rows 2 and 3
     return x;
+}
+__device__ __forceinline__ double last_lane(double x)
+{
+    const int2 w = __builtin_bit_cast(int2, x);
+    return __builtin_bit_cast(double, int2{__builtin_amdgcn_readlane(w.x, 63), __builtin_amdgcn_readlane(w.y, 63)});
 }
 
 // Sums of the gates up to each token, in scan order and in powers of two, and the strengths: every wave its own (a lane a token).  Differences of
@@ -54,15 +73,21 @@ struct Gates {
         g = load_element<T>(chunk_rows(gates, s, b, h, s.H, 1, chunk), at);
         beta = load_element<T>(chunk_rows(strengths, s, b, h, s.H, 1, chunk), at);
     }
-    __device__ __forceinline__ double sum(int lane) const
+    __device__ __forceinline__ double sum() const
     {
         const double kLog2e = 1.4426950408889634074;
-        return wave_prefix(kLog2e * double(fmaxf(value(g), kGateFloor)), lane);
+        return wave_prefix(kLog2e * double(fmaxf(value(g), kGateFloor)));
     }
     __device__ __forceinline__ float strength() const { return kBwd ? beta_divisor(value(beta)) : value(beta); }
 };
 
 __device__ __forceinline__ float exp2_of(double x) { return fast_exp2(float(x)); }
+// decay from token c to token t, both the sums up to them, 1 for pairs that are none (formed for these as well: a branch for each costs more)
+__device__ __forceinline__ float decay_of(double t, double c, bool pair)
+{
+    const float x = float(t - c);
+    return fast_exp2(pair ? x : 0.f);
+}
 
 // Rows of a chunk in LDS, as they are, for fragments of rows and of columns
 template <typename T, int DK>
@@ -126,7 +151,7 @@ __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
     }
     requests_stay();
     {
-        const double p = gates.sum(lane), total = __shfl(p, 63);
+        const double p = gates.sum(), total = last_lane(p);
         const float beta = gates.strength();
         sum[w][lane] = p;
         bet[w][lane] = beta;
@@ -179,7 +204,7 @@ __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
         for (int i = 0; i < 4; ++i) {
             const int t = 16 * w + 4 * g + i, c = 16 * n + r;
             // (factors of 0 and 1 rather than branches)
-            const float decay = exp2_of(c <= t ? sum[w][t] - sum[w][c] : 0.0) * bet[w][c];
+            const float decay = decay_of(sum[w][t], sum[w][c], c <= t) * bet[w][c];
             inv[t * kPitch + c] = (c < t ? 1.f : 0.f) * decay * kk[n][i];
             sco[t * kPitch + c] = (c <= t ? 1.f : 0.f) * decay * qk[n][i];
         }
