@@ -405,7 +405,7 @@ __device__ __forceinline__ float dot(const Full &a, const Full &b, float acc)
 // time is mostly that of its trips to memory.  The contractions over value columns take kSlice of them at a time.
 // kOne: the values are one slice; two workgroups then fit a compute unit's registers (without it the accumulators are live across the
 // requests of the next slice, and what spills costs more than the second workgroup brings).
-template <typename T, int DK, bool kOne>
+template <typename T, int DK, bool kOne, bool kSingle>
 __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) void gd_gradients(GradientArgs<T> a)
 {
     using In = typename operands<T, 2>::In;
@@ -486,21 +486,21 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
 #pragma unroll
     for (int ct = 0; ct < kCt; ++ct) dq[ct] = dk[ct] = zero;
 
-    for (int h = hk * share; h < (hk + 1) * share; ++h) {
+    for (int h = hk * share; h < hk * share + (kSingle ? 1 : share); ++h) {
         // (addresses are formed from here on in every turn: formed once for all, they would be more than the registers hold)
-        asm volatile("" : "+v"(lane));
+        if (!kSingle) asm volatile("" : "+v"(lane));
         r = lane & 15, g = lane >> 4;
-        f32x4 x[4], y[4], read[kCt], erase[kCt], write[kCt];
-#pragma unroll
-        for (int n = 0; n < 4; ++n) x[n] = y[n] = zero;
-#pragma unroll
-        for (int ct = 0; ct < kCt; ++ct) read[ct] = erase[ct] = write[ct] = zero;
-        if (h > hk * share) {
+        if (!kSingle && h > hk * share) {
             request_gates(h);
             request_slice(h, 0);
             requests_stay();
             put_gates();
         }
+        f32x4 x[4], y[4], read[kCt], erase[kCt], write[kCt];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) x[n] = y[n] = zero;
+#pragma unroll
+        for (int ct = 0; ct < kCt; ++ct) read[ct] = erase[ct] = write[ct] = zero;
         float ds = 0.f;  // <D, S>
         for (int v0 = 0; v0 < (kOne ? 1 : blocks); v0 += kVs) {
             if (!kOne && v0 > 0) {
@@ -708,10 +708,12 @@ hipError_t launch(const Shape &s, const GradientPointers &p, void *workspace, hi
     gd_both_chains<T, DK, N><<<dim3((slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 2), 128, 0, stream>>>(chain, adjoint);
     const unsigned key_units = unsigned(s.B) * unsigned(s.Hk) * unsigned(s.chunks);
     constexpr size_t lds = gradient_lds<T, DK>();
-    if (s.dv <= (DK <= 64 ? 64 : 32))
-        gd_gradients<T, DK, true><<<key_units, 256, lds, stream>>>(gradient);
+    if (s.dv > (DK <= 64 ? 64 : 32))
+        gd_gradients<T, DK, false, false><<<key_units, 256, lds, stream>>>(gradient);
+    else if (s.H > s.Hk)
+        gd_gradients<T, DK, true, false><<<key_units, 256, lds, stream>>>(gradient);
     else
-        gd_gradients<T, DK, false><<<key_units, 256, lds, stream>>>(gradient);
+        gd_gradients<T, DK, true, true><<<key_units, 256, lds, stream>>>(gradient);
     return hipGetLastError();
 }
 
