@@ -10,6 +10,8 @@ namespace {
 
 using namespace gd;
 
+constexpr unsigned kComputeUnits = 256;
+
 // Parts of a 32-bit operand: a returned state takes three, bf16 results two
 template <typename T, int DK>
 size_t fwd_bytes(const Shape &s, bool states)
@@ -30,7 +32,13 @@ hipError_t launch(const Shape &s, const void *q, const void *k, const void *v, c
     const ChainArgs<T> c = {s, p.q, p.k, static_cast<const T *>(v), initial, static_cast<T *>(out), final_state, nullptr, nullptr, ws, key_ws};
     const LaunchTimer timer(kKernelGatedDelta, stream);
     gd_prepare<T, DK, N, false><<<units, 256, 0, stream>>>(p);
-    gd_states<T, DK, N><<<(slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 128, 0, stream>>>(c);
+    // 128 channels are two waves' while every workgroup has a compute unit to itself (2 x 16 heads of 8191 tokens, bf16: 340 -> 312 us; 2 x 4 of
+    // 2048, fp32: 192 -> 150), and one wave's behind that (8 x 16 heads, 2048 tokens in bf16: 289 -> 282; 1024 in fp32: 330 -> 294)
+    const unsigned blocks = (slabs + 7) / 8 * 8 * unsigned(s.dv / 16);
+    if (DK == 128 && slabs * unsigned(s.dv / 16) <= kComputeUnits)
+        gd_states<T, DK, N, DK == 128 ? 2 : 1><<<blocks, 192, 0, stream>>>(c);
+    else
+        gd_states<T, DK, N, 1><<<blocks, 128, 0, stream>>>(c);
     return hipGetLastError();
 }
 

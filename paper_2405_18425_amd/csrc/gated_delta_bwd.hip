@@ -327,14 +327,14 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
 
 // Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'
 template <typename T, int DK, int N>
-__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(chain_waves<T, DK>, chain_waves<T, DK>))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
+__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(chain_waves<T, DK, 1>, chain_waves<T, DK, 1>))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
 {
     __shared__ __align__(16) unsigned char lds[AdjointLds<DK>::bytes], scal[kScalarBytes + Strip<T>::bytes], own[2 * kScalarBytes + Strip<T>::bytes];
     Columns at;
     if (!columns_of(a.s, at)) return;
     if (blockIdx.y == 0) {
         if (threadIdx.x < 64)
-            states<T, DK, N, true>(c, at, scal, lds);
+            states<T, DK, N, true, 1>(c, at, 0, scal, lds, nullptr);
         else
             emit_states<T, DK>(c, at, lds);
     } else {

@@ -206,16 +206,18 @@ __device__ __forceinline__ void tile_row(float (&x)[8], const unsigned char *lds
     for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const float *>(lds + 4 * ((8 * group + j) * Tile<kRows>::pitch + row));
 }
 
-template <typename T, int DK, int N, bool kBwd>
-__device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at, unsigned char *scal /* the wave's: scalars, then a strip */,
-                                       unsigned char *lds /* two HandOvers, or two state and two token tiles */)
+// kWaves waves share the chain of 16 columns, each with its channels of the state: one exchange a chunk, of the sums over channels; e is formed by each
+template <typename T, int DK, int N, bool kBwd, int kWaves>
+__device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at, int wave, unsigned char *scal /* the wave's: scalars, then a strip */,
+                                       unsigned char *lds /* two HandOvers, or two state and two token tiles */, unsigned char *sums /* of two chunks */)
 {
     using In = typename operands<T, N>::In;
     using Mid = typename operands<T, N>::Mid;
     using Ws = ChunkWs<T, N, kBwd>;
     using Kw = KeyWs<T, DK, kBwd>;
     using Hand = HandOver<T, DK>;
-    constexpr int kKs = DK / 32, kCt = DK / 16;
+    constexpr int kKs = DK / 32 / kWaves, kCt = DK / 16 / kWaves;
+    const int ks0 = wave * kKs, ct0 = wave * kCt;
     const Shape &s = a.s;
     const int lane = at.lane, r = at.r, g = at.g, col = at.col;
     const unsigned slab = at.slab;
@@ -228,7 +230,7 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
     const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk);
     unsigned key_at[4], value_at[Strip<T>::loads];
 #pragma unroll
-    for (int m = 0; m < 4; ++m) key_at[m] = row_offset<T>(key_pitch, token_at(s, paired(m, r)), 0, g, s.dk);
+    for (int m = 0; m < 4; ++m) key_at[m] = row_offset<T>(key_pitch, token_at(s, paired(m, r)), ks0, g, s.dk);
 #pragma unroll
     for (int l = 0; l < Strip<T>::loads; ++l) value_at[l] = strip_offset<T>(s, pitch_of<T>(s, s.H, s.dv), col >> 4, lane, l);
 
@@ -240,7 +242,7 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) S[ct][i] = load4(from0, state_offset(s, ct, i, g, col));
+            for (int i = 0; i < 4; ++i) S[ct][i] = load4(from0, state_offset(s, ct0 + ct, i, g, col));
     }
 
     const int first = chunk_at(s, 0), move = s.reverse ? -1 : 1;
@@ -273,7 +275,7 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int ct = 0; ct < kCt; ++ct) fkt[ct][ks] = get<In>(from0, 0, 2 * ct + ks, lane);
+            for (int ct = 0; ct < kCt; ++ct) fkt[ct][ks] = get<In>(from0, 0, 2 * (ct0 + ct) + ks, lane);
     };
     // (in the order of the loop: its waits count the requests behind the one they are for, and hold for the way into the loop as well)
     load_first();
@@ -291,7 +293,7 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
         if constexpr (kBwd) {
             __syncthreads();
 #pragma unroll
-            for (int ct = 0; ct < kCt; ++ct) tile_put<DK>(hand, ct, r, g, S[ct]);
+            for (int ct = 0; ct < kCt; ++ct) tile_put<DK>(hand, ct0 + ct, r, g, S[ct]);
         }
         strip_put(scal + kScalarBytes, v, lane);
         share_scalars(scal, raw, lane);
@@ -302,7 +304,7 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) {
             fs[ks] = from<Mid>(S[2 * ks], S[2 * ks + 1]);
-            if constexpr (!kBwd) lds_put(hand, ks, lane, first_parts<N, 2>(fs[ks]));
+            if constexpr (!kBwd) lds_put(hand, ks0 + ks, lane, first_parts<N, 2>(fs[ks]));
         }
         f32x4 e[4];
 #pragma unroll
@@ -313,6 +315,14 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
         requests_stay();
         load_keys();
         requests_stay();
+        if constexpr (kWaves == 2) {
+            unsigned char *mine = sums + 4096 * (2 * (step & 1) + wave), *other = sums + 4096 * (2 * (step & 1) + 1 - wave);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4 *>(mine + 1024 * m + 16 * lane) = e[m];
+            __syncthreads();
+#pragma unroll
+            for (int m = 0; m < 4; ++m) e[m] += *reinterpret_cast<const f32x4 *>(other + 1024 * m + 16 * lane);
+        }
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
             T x[8];
@@ -336,7 +346,9 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
         const float whole = whole_decay(scal);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            if constexpr (kBwd)
+            if (wave > 0)
+                ;
+            else if constexpr (kBwd)
                 tile_put<kC>(hand + Tile<DK>::bytes, m, r, g, e[m]);
             else
                 *reinterpret_cast<f32x4 *>(hand + Hand::e + 1024 * m + 16 * lane) = e[m];
@@ -359,7 +371,7 @@ __device__ __forceinline__ void states(const ChainArgs<T> &a, const Columns &at,
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) store4(to, state_offset(s, ct, i, g, col), S[ct][i]);
+            for (int i = 0; i < 4; ++i) store4(to, state_offset(s, ct0 + ct, i, g, col), S[ct][i]);
     }
 }
 
@@ -398,7 +410,7 @@ __device__ __forceinline__ void emit_states(const ChainArgs<T> &a, const Columns
 }
 
 // The outputs of a wave's columns, one chunk behind the chain
-template <typename T, int DK, int N>
+template <typename T, int DK, int N, int kWaves>
 __device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at, unsigned char *own /* the wave's: scalars, then a tile */, const unsigned char *lds)
 {
     using In = typename operands<T, N>::In;
@@ -440,6 +452,7 @@ __device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at
     requests_stay();
     load_scores();
     requests_stay();
+    if (kWaves == 2) __syncthreads();
     for (int step = 0; step < s.chunks; ++step) {
         const Rsrc out = to.here();
         to.next();
@@ -461,6 +474,7 @@ __device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at
         requests_stay();
         load_queries();
         requests_stay();
+        if (kWaves == 2 && step + 1 < s.chunks) __syncthreads();  // (the chain's waves exchange the next chunk's sums)
         const Mid2 fe[2] = {from<Mid2>(e[0], e[1]), from<Mid2>(e[2], e[3])};
 #pragma unroll
         for (int m = 0; m < 4; ++m) o[m] *= scalars(own, kC0, m, g);
@@ -483,20 +497,22 @@ __device__ __forceinline__ void outputs(const ChainArgs<T> &a, const Columns &at
 }
 
 // Waves on a SIMD: two where their registers fit
-template <typename T, int DK>
-constexpr int chain_waves = DK * int(sizeof(T)) <= 128 ? 2 : 1;
+template <typename T, int DK, int kWaves>
+constexpr int chain_waves = DK / kWaves * int(sizeof(T)) <= 128 ? 2 : 1;
 
-// Two waves per 16 columns: the chain, and the outputs one chunk behind it
-template <typename T, int DK, int N>
-__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(chain_waves<T, DK>, chain_waves<T, DK>))) void gd_states(ChainArgs<T> a)
+// The waves of a chain, and one for the outputs, a chunk behind
+template <typename T, int DK, int N, int kWaves>
+__global__ __launch_bounds__(64 * (kWaves + 1)) __attribute__((amdgpu_waves_per_eu(chain_waves<T, DK, kWaves>, chain_waves<T, DK, kWaves>))) void gd_states(ChainArgs<T> a)
 {
-    __shared__ __align__(16) unsigned char lds[2 * HandOver<T, DK>::bytes], scal[kScalarBytes + Strip<T>::bytes], own[kScalarBytes + Tile<kC>::bytes];
+    __shared__ __align__(16) unsigned char lds[2 * HandOver<T, DK>::bytes], scal[kWaves][kScalarBytes + Strip<T>::bytes], own[kScalarBytes + Tile<kC>::bytes],
+        sums[kWaves == 2 ? 4 * 4096 : 16];
     Columns at;
     if (!columns_of(a.s, at)) return;
-    if (threadIdx.x < 64)
-        states<T, DK, N, false>(a, at, scal, lds);
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
+    if (wave < kWaves)
+        states<T, DK, N, false, kWaves>(a, at, wave, scal[wave], lds, sums);
     else
-        outputs<T, DK, N>(a, at, own, lds);
+        outputs<T, DK, N, kWaves>(a, at, own, lds);
 }
 
 }  // namespace gd

@@ -406,8 +406,8 @@ int delta_shape_status(int B, int H, int Hk, int L, int dk, int dv, int dtype)
     if (dtype != VIG_F32 && dtype != VIG_BF16) return VIG_ERR_DTYPE;
     if (!delta_width_ok(dk) || !delta_width_ok(dv) || H % Hk != 0) return VIG_ERR_UNSUPPORTED;
     // rows of a chunk are addressed with 32 bits, and a head's 64-token chunks and 16-column parts are workgroups; the
-    // workspace of the gradient is under 64 bytes per token and channel
-    if (!sizes_ok(B, H, L, 64L * (dk > dv ? dk : dv)) || H >= (1 << 15) || L >= 0x7fffff00) return VIG_ERR_SHAPE;
+    // workspace of the gradient is under 128 bytes per token and channel
+    if (!sizes_ok(B, H, L, 128L * (dk > dv ? dk : dv)) || H >= (1 << 15) || L >= 0x7fffff00) return VIG_ERR_SHAPE;
     if ((long(B) * H + 7) * ((long(L) + 63) / 64) > 0x7fffffffL || (long(B) * H + 7) * 8 > 0x7fffffffL) return VIG_ERR_SHAPE;
     return VIG_OK;
 }
