@@ -349,8 +349,8 @@ int gated_delta_fwd(const void *q, const void *k, const void *v, const void *g, 
  *   d_out [B, H, L, dv]; d_final_state [B, H, dk, dv] FP32 or NULL (zero)                    in
  *   dq, dk [B, Hk, L, dk] (summed over the heads that share a key head), dv [B, H, L, dv], dg, dbeta [B, H, L]      out
  *   d_initial_state [B, H, dk, dv] FP32 or NULL (not wanted)                                 out
- *   workspace: at least gated_delta_bwd_workspace_bytes(...) bytes (the chunks' matrices, two states per chunk, two fp32
- *   rows of dv values per token).  Results do not depend on how the work is spread: no atomics.
+ *   workspace: at least gated_delta_bwd_workspace_bytes(...) bytes (the chunks' matrices; two states a chunk and two rows
+ *   of dv values a token, 32 bits an element).  Results do not depend on how the work is spread: no atomics.
  */
 size_t gated_delta_bwd_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, int dtype);
 int gated_delta_bwd(const void *q, const void *k, const void *v, const void *g, const void *beta, const void *initial_state,

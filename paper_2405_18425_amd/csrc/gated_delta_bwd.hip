@@ -325,7 +325,8 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
     take(0);
 }
 
-// Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'
+// Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'.  8 x 6 heads of 4096 tokens (bf16, 64 x 64): 172 us for 167 MB in and
+// 223 MB out; one chain after the other 87 + 129 us.  A load a line two chunks ahead, to have them in L2, costs more (197 us) than it saves.
 template <typename T, int DK, int N>
 __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(chain_waves<T, DK, 1>, chain_waves<T, DK, 1>))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
 {
@@ -404,7 +405,9 @@ __device__ __forceinline__ float dot(const Full &a, const Full &b, float acc)
 // the rows of S and D -- each requests a quarter of and all read from LDS; every request of a turn stands before its first wait, since a workgroup's
 // time is mostly that of its trips to memory.  The contractions over value columns take kSlice of them at a time.
 // kOne: the values are one slice; two workgroups then fit a compute unit's registers (without it the accumulators are live across the
-// requests of the next slice, and what spills costs more than the second workgroup brings).
+// requests of the next slice, and what spills costs more than the second workgroup brings).  kSingle: no other value head shares the keys; without the
+// loop nothing spills (8 x 6 heads of 4096 tokens 85 us, 106 with it; 8 x 16 heads on 8 key heads, 2048 tokens, need it: 112 us with two workgroups a
+// compute unit and 17 registers spilled, 157 with one and none).
 template <typename T, int DK, bool kOne, bool kSingle>
 __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) void gd_gradients(GradientArgs<T> a)
 {

@@ -2,7 +2,13 @@
 //
 // The chain's wave holds its columns of the state in accumulators (32-bit) and takes a chunk's matrices from the workspace as fragments, 16 bytes
 // a lane, each requested for the next chunk as soon as its last product of this chunk has been issued.  The three products of a step
-// follow each other in registers; only what the outputs need goes through LDS, with one barrier a chunk.  Columns of one head sit on one XCD (blockIdx % 8), whose L2 they read the fragments from.
+// follow each other in registers; only what the outputs need goes through LDS, with one barrier a chunk.  Columns of one head sit on one
+// XCD (blockIdx % 8), whose L2 they read the fragments from.
+//
+// What bounds it (64 x 64, bf16): where every workgroup has a compute unit, its own instructions, 50 matrix and 225 vector ones a chunk in one wave, 1.1 us
+// (8 x 6 heads of 4096 tokens: 70 us; 66 without a request in the loop, 63 without the outputs' either).  With several workgroups on a compute unit, what
+// comes through its first-level cache, 50 KB a chunk and 16 columns: 16 x 16 heads of 1024 tokens take 79 us, 35 without requests.  Two groups of columns
+// in a wave take twice as long a step; two in a workgroup read the same lines at different times (115 us instead of 74).
 #pragma once
 
 #include "gated_delta.hpp"

