@@ -79,7 +79,8 @@ struct Gates {
     __device__ __forceinline__ double sum() const
     {
         const double kLog2e = 1.4426950408889634074;
-        return wave_prefix(kLog2e * double(fmaxf(value(g), kGateFloor)));
+        const float x = value(g);
+        return wave_prefix(kLog2e * double(x < kGateFloor ? kGateFloor : x));  // (a NaN stays one)
     }
     __device__ __forceinline__ float strength() const { return kBwd ? beta_divisor(value(beta)) : value(beta); }
 };

@@ -116,6 +116,35 @@ def test_delta_special_inputs(dtype, kind):
         assert torch.equal(whole, part)
 
 
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("B,H,Hk,L", ((1, 4, 4, 700), (2, 2, 1, 129), (5, 8, 4, 330)))
+def test_delta_wide_heads_few_and_many(dtype, B, H, Hk, L):
+    """128 channels, 32 to 320 workgroups of 16 columns: a chain is two waves' or one wave's"""
+    print(f"delta {dtype} {B} {H} {Hk} {L}", flush=True)
+    t = _delta(B, H, Hk, L, 128, 128, dtype, states=B != 2, seed=L)
+    _check_delta(t, dtype, "bhld", "forward" if B == 1 else "backward", f"{B} x {H} heads of {L}")
+
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+def test_delta_nan_gate_reaches_its_head_only(dtype):
+    from paper_2405_18425_amd import binding as vb
+
+    t = _delta(2, 3, 3, 200, 64, 64, dtype)
+    args = [t[x] for x in ("q", "k", "v", "g", "beta")]
+    clean, fin = vb.gated_delta_fwd(*args, initial_state=t["s0"], return_final_state=True)
+    t["g"][1, 1, 70] = float("nan")
+    out, nan_fin = vb.gated_delta_fwd(*args, initial_state=t["s0"], return_final_state=True)
+    others = [(b, h) for b in range(2) for h in range(3) if (b, h) != (1, 1)]
+    for b, h in others:
+        assert torch.equal(out[b, h], clean[b, h]) and torch.equal(nan_fin[b, h], fin[b, h])
+    assert torch.equal(out[1, 1, :64], clean[1, 1, :64])
+    assert torch.isnan(out[1, 1, 70:]).all() and torch.isnan(nan_fin[1, 1]).all()
+    grads = vb.gated_delta_bwd(*args, t["d_out"], initial_state=t["s0"])
+    for g in grads[:5]:
+        assert all(torch.isfinite(g[b, h]).all() for b, h in others)
+    assert torch.isnan(grads[0][1, 1]).any()
+
+
 def test_delta_continues_from_a_state_in_place():
     from paper_2405_18425_amd import binding as vb
 
