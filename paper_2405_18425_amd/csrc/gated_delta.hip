@@ -13,12 +13,11 @@ using namespace gd;
 constexpr unsigned kComputeUnits = 256;
 
 // Parts of a 32-bit operand: a returned state takes three, bf16 results two
-template <typename T, int DK>
-size_t fwd_bytes(const Shape &s, bool states)
+template <typename T, int DK, int N>
+size_t matrix_bytes(const Shape &s)
 {
     const size_t units = size_t(s.B) * s.H * s.chunks, key_units = size_t(s.B) * s.Hk * s.chunks;
-    const size_t chunk = states ? ChunkWs<T, 3, false>::bytes : ChunkWs<T, 2, false>::bytes;
-    return round256(units * chunk) + round256(key_units * KeyWs<T, DK, false>::bytes);
+    return round256(units * ChunkWs<T, N, false>::bytes) + round256(key_units * KeyWs<T, DK, false>::bytes);
 }
 
 template <typename T, int DK, int N>
@@ -28,7 +27,8 @@ hipError_t launch(const Shape &s, const void *q, const void *k, const void *v, c
     const unsigned slabs = unsigned(s.B) * unsigned(s.H), units = slabs * unsigned(s.chunks);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     unsigned char *key_ws = ws + round256(size_t(units) * ChunkWs<T, N, false>::bytes);
-    const PrepareArgs<T> p = {s, static_cast<const T *>(q), static_cast<const T *>(k), static_cast<const T *>(g), static_cast<const T *>(beta), ws, key_ws};
+    const PrepareArgs<T> p = {s, static_cast<const T *>(q), static_cast<const T *>(k), static_cast<const T *>(g), static_cast<const T *>(beta), ws, key_ws,
+                               matrix_bytes<T, DK, N>(s) > kStreamedBytes};
     const ChainArgs<T> c = {s, p.q, p.k, static_cast<const T *>(v), initial, static_cast<T *>(out), final_state, nullptr, nullptr, ws, key_ws};
     const LaunchTimer timer(kKernelGatedDelta, stream);
     gd_prepare<T, DK, N, false><<<units, 256, 0, stream>>>(p);
@@ -65,7 +65,7 @@ size_t gated_delta_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, 
     const Shape s = {B, H, Hk, L, dk, dv, (L + kC - 1) / kC, false, false};
     const auto of = [&](auto t) {
         using T = decltype(t);
-        return dk <= 32 ? fwd_bytes<T, 32>(s, true) : dk <= 64 ? fwd_bytes<T, 64>(s, true) : fwd_bytes<T, 128>(s, true);
+        return dk <= 32 ? matrix_bytes<T, 32, 3>(s) : dk <= 64 ? matrix_bytes<T, 64, 3>(s) : matrix_bytes<T, 128, 3>(s);
     };
     return is_bf16 ? of(bf16_t{}) : of(float{});
 }

@@ -248,15 +248,25 @@ template <typename Frag>
 constexpr int planes = int(sizeof(Frag)) / 16;
 template <typename Frag>
 constexpr size_t frag_bytes = size_t(planes<Frag>) * 1024;
+constexpr int kStream = 2;  // a non-temporal store
 template <typename Frag>
-__device__ __forceinline__ void put(Rsrc ws, size_t first, int block, int lane, const Frag &f)
+__device__ __forceinline__ void put(Rsrc ws, size_t first, int block, int lane, const Frag &f, bool stream)
 {
     u32x4 w[planes<Frag>];
     __builtin_memcpy(w, &f, sizeof(f));
 #pragma unroll
-    for (int i = 0; i < planes<Frag>; ++i)
-        __builtin_amdgcn_raw_buffer_store_b128(w[i], ws, 16u * unsigned(lane), unsigned(first) + unsigned(block * planes<Frag> + i) * 1024u, 0);
+    for (int i = 0; i < planes<Frag>; ++i) {
+        const unsigned at = unsigned(first) + unsigned(block * planes<Frag> + i) * 1024u;
+        if (stream)
+            __builtin_amdgcn_raw_buffer_store_b128(w[i], ws, 16u * unsigned(lane), at, kStream);
+        else
+            __builtin_amdgcn_raw_buffer_store_b128(w[i], ws, 16u * unsigned(lane), at, 0);
+    }
 }
+// Matrices of more than half the Infinity Cache's 256 MB are written around the caches: little of them would be there when the chains come to it, and what
+// they take would be another's.  (8 x 6 heads of 4096 tokens, gradient, 163 MB: matrices 40 -> 36 us, chains 175 -> 170; 2 x 16 heads of 8191,
+// 128 x 128, 160 MB: chains 308 -> 298.  Below it costs: 8 x 6 of 4096 forward, 101 MB: chains 70 -> 80; 64 x 6 of 196, gradient, 81 MB: 48 -> 66.)
+constexpr size_t kStreamedBytes = size_t(128) << 20;
 template <typename Frag>
 __device__ __forceinline__ Frag get(Rsrc ws, size_t first, int block, int lane)
 {

@@ -701,7 +701,7 @@ hipError_t launch(const Shape &s, const GradientPointers &p, void *workspace, hi
     const T *q = static_cast<const T *>(p.q), *k = static_cast<const T *>(p.k), *v = static_cast<const T *>(p.v), *g = static_cast<const T *>(p.g),
             *beta = static_cast<const T *>(p.beta), *d_out = static_cast<const T *>(p.d_out);
     unsigned char *S = ws + at.states, *D = ws + at.adjoints, *e = ws + at.wrong, *r = ws + at.r;
-    const PrepareArgs<T> prepare = {s, q, k, g, beta, ws, ws + at.key_ws};
+    const PrepareArgs<T> prepare = {s, q, k, g, beta, ws, ws + at.key_ws, at.states > kStreamedBytes};
     const ChainArgs<T> chain = {s, q, k, v, p.initial, nullptr, nullptr, S, e, ws, ws + at.key_ws};
     const AdjointArgs<T> adjoint = {s, k, d_out, p.d_final, static_cast<T *>(p.dv), p.d_initial, D, r, ws, ws + at.key_ws};
     const GradientArgs<T> gradient = {s, q, k, g, beta, d_out, static_cast<T *>(p.dq), static_cast<T *>(p.dk), static_cast<T *>(p.dg),

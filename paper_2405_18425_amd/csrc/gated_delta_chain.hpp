@@ -162,7 +162,9 @@ __device__ __forceinline__ void strip_column(float (&x)[8], const unsigned char 
 }
 
 // What the chains of the gradient leave: a state (DK rows) or 64 tokens' rows, 16 columns a wave, first in LDS as [column][row] tiles of floats, which a
-// second wave takes to the workspace as fragments of two parts: rows by 16 in tiles, columns along the products.
+// second wave takes to the workspace as fragments of two parts: rows by 16 in tiles, columns along the products.  By non-temporal stores: read by the
+// next launch only, they leave the L2 to the fragments that the columns of a head share (chains of 8 x 6 heads of 4096 tokens 185 -> 173 us, 64 x 6 of 196
+// 54.5 -> 48).
 template <int kRows>
 struct Tile {
     static constexpr int pitch = kRows + 4, bytes = 16 * pitch * 4;
@@ -187,10 +189,6 @@ struct Place {
 };
 __device__ __forceinline__ Place natural(int row) { return {row >> 4, row & 15}; }
 __device__ __forceinline__ Place unpaired(int row) { return {2 * (row >> 5) + ((row >> 2) & 1), 4 * ((row >> 3) & 3) + (row & 3)}; }
-
-// Written once and read by the next launch: marked non-temporal, it leaves the L2 to the fragments that the columns of a head share (chains of 8 x 6 heads
-// of 4096 tokens 185 -> 173 us, 64 x 6 of 196 54.5 -> 48).
-constexpr int kStream = 2;
 
 // eight columns of a row as a fragment's lane (of a head whose last block has 16 columns, the other half is not written: who reads it leaves it out)
 template <typename Mid2>

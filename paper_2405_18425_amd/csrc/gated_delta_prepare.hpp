@@ -19,6 +19,7 @@ struct PrepareArgs {
     Shape s;
     const T *q, *k, *g, *beta;
     unsigned char *ws, *key_ws;
+    bool stream;  // see kStreamedBytes
 };
 
 constexpr int kPitch = 68;  // floats of a row of a 64 x 64 tile in LDS: 16-byte rows, four banks further each
@@ -182,10 +183,10 @@ __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
             const int block = 4 * o + w;
             In f;
             key_column<DK>(f, shared, block >> 1, block & 1, r, g);
-            put(kw, 0, block, lane, f);
+            put(kw, 0, block, lane, f, a.stream);
             if constexpr (kBwd) {
                 key_column<DK>(f, shared + KeyTile<T, DK>::bytes, block >> 1, block & 1, r, g);
-                put(kw, Kw::blocks * frag_bytes<In>, block, lane, f);
+                put(kw, Kw::blocks * frag_bytes<In>, block, lane, f, a.stream);
             }
         }
     }
@@ -273,18 +274,18 @@ __global__ __launch_bounds__(256) void gd_prepare(PrepareArgs<T> a)
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
         const int c = 32 * ks + 8 * g;
-        if (ks <= (w >> 1)) put(ws, Ws::inverse, lower_block(w, ks), lane, from<Mid>(inv + tr * kPitch + c));
+        if (ks <= (w >> 1)) put(ws, Ws::inverse, lower_block(w, ks), lane, from<Mid>(inv + tr * kPitch + c), a.stream);
         if constexpr (!kBwd) {
-            if (ks <= (w >> 1)) put(ws, Ws::scores, lower_block(w, ks), lane, from<MidP>(sco + tr * kPitch + c));
+            if (ks <= (w >> 1)) put(ws, Ws::scores, lower_block(w, ks), lane, from<MidP>(sco + tr * kPitch + c), a.stream);
         } else if (ks >= (w >> 1)) {
             float x[8], p[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = inv[(c + j) * kPitch + tr], p[j] = sco[(c + j) * kPitch + tr];
             Mid f;
             make(f, x);
-            put(ws, Ws::inverse + kTriBlocks * frag_bytes<Mid>, upper_block(w, ks), lane, f);
+            put(ws, Ws::inverse + kTriBlocks * frag_bytes<Mid>, upper_block(w, ks), lane, f, a.stream);
             make(f, p);
-            put(ws, Ws::scores, upper_block(w, ks), lane, f);
+            put(ws, Ws::scores, upper_block(w, ks), lane, f, a.stream);
         }
     }
 }
