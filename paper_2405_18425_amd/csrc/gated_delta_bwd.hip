@@ -325,7 +325,7 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
     take(0);
 }
 
-// Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'.  8 x 6 heads of 4096 tokens (bf16, 64 x 64): 172 us for 167 MB in and
+// Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'.  8 x 6 heads of 4096 tokens (bf16, 64 x 64): 170 us for 167 MB in and
 // 223 MB out; one chain after the other 87 + 129 us.  A load a line two chunks ahead, to have them in L2, costs more (197 us) than it saves.
 template <typename T, int DK, int N>
 __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(chain_waves<T, DK, 1>, chain_waves<T, DK, 1>))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
