@@ -402,11 +402,12 @@ __device__ __forceinline__ float dot(const Full &a, const Full &b, float acc)
 }
 
 // One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  What more than one wave needs -- rows of k, K^T and Q^T, e,
-// the rows of S and D -- each requests a quarter of and all read from LDS; every request of a turn stands before its first wait, since a workgroup's
-// time is mostly that of its trips to memory.  The contractions over value columns take kSlice of them at a time.
+// the rows of S and D -- each requests a quarter of and all read from LDS; every request of a turn stands before its first wait: one trip to memory
+// a turn.  The contractions over value columns take kSlice of them at a time.  Bound by the instructions of two waves a SIMD (64 x 64, bf16: 1350 vector and 168
+// matrix ones each): workgroups that go on to another chunk with its requests under way take 90 us where these take 81.
 // kOne: the values are one slice; two workgroups then fit a compute unit's registers (without it the accumulators are live across the
 // requests of the next slice, and what spills costs more than the second workgroup brings).  kSingle: no other value head shares the keys; without the
-// loop nothing spills (8 x 6 heads of 4096 tokens 85 us, 106 with it; 8 x 16 heads on 8 key heads, 2048 tokens, need it: 112 us with two workgroups a
+// loop nothing spills (8 x 6 heads of 4096 tokens 81 us, 106 with it; 8 x 16 heads on 8 key heads, 2048 tokens, need it: 112 us with two workgroups a
 // compute unit and 17 registers spilled, 157 with one and none).
 template <typename T, int DK, bool kOne, bool kSingle>
 __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) void gd_gradients(GradientArgs<T> a)
