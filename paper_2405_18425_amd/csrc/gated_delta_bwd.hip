@@ -381,24 +381,20 @@ __device__ __forceinline__ Frag get_at(Rsrc ws, unsigned at, int block, int lane
     __builtin_memcpy(&f, w, sizeof(f));
     return f;
 }
-// sum of the products of the lanes' values, added to acc
-__device__ __forceinline__ float dot(const Parts<2> &a, const Parts<2> &b, float acc)
+// The sum of products of the rows of two tiles, in parts: the matrix cores' products of every row with every row, of which the diagonal is wanted (two
+// instructions a part where unpacking and adding up takes eighty); 32-bit values one by one.
+__device__ __forceinline__ void inner(f32x4 &acc, const Parts<2> &a, const Parts<2> &b) { mma(acc, a, b); }
+__device__ __forceinline__ void inner(f32x4 &acc, const Full &a, const Full &b)
 {
-    u32x4 x[2], y[2];
-    __builtin_memcpy(x, &a, sizeof(a));
-    __builtin_memcpy(y, &b, sizeof(b));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        acc = fmaf(bf16_lo_to_f32(x[0][j]) + bf16_lo_to_f32(x[1][j]), bf16_lo_to_f32(y[0][j]) + bf16_lo_to_f32(y[1][j]), acc);
-        acc = fmaf(bf16_hi_to_f32(x[0][j]) + bf16_hi_to_f32(x[1][j]), bf16_hi_to_f32(y[0][j]) + bf16_hi_to_f32(y[1][j]), acc);
-    }
-    return acc;
+    for (int j = 0; j < 8; ++j) acc[0] = fmaf(a.v[j], b.v[j], acc[0]);
 }
-__device__ __forceinline__ float dot(const Full &a, const Full &b, float acc)
+template <typename Frag>
+__device__ __forceinline__ float of_lane(const f32x4 &acc, int r, int g)
 {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc = fmaf(a.v[j], b.v[j], acc);
-    return acc;
+    if constexpr (std::is_same<Frag, Full>::value) return acc[0];
+    const float x = (r & 2) ? ((r & 1) ? acc[3] : acc[2]) : ((r & 1) ? acc[1] : acc[0]);
+    return (r >> 2) == g ? x : 0.f;
 }
 
 // One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  What more than one wave needs -- rows of k, K^T and Q^T, e,
@@ -505,7 +501,7 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
         for (int n = 0; n < 4; ++n) x[n] = y[n] = zero;
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) read[ct] = erase[ct] = write[ct] = zero;
-        float ds = 0.f;  // <D, S>
+        f32x4 inners = zero;  // <D, S>
         for (int v0 = 0; v0 < (kOne ? 1 : blocks); v0 += kVs) {
             if (!kOne && v0 > 0) {
                 request_slice(h, v0);
@@ -516,7 +512,7 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
 #pragma unroll
             for (int o = 0; o < kOwn; ++o)
                 if (kCt * kVs % 4 == 0 || 4 * o + w < kCt * kVs) {
-                    ds = dot(fs[o], fd[o], ds);
+                    inner(inners, fd[o], fs[o]);
                     lds_put(fS, 4 * o + w, lane, fs[o]);
                     lds_put(fD, 4 * o + w, lane, fd[o]);
                 }
@@ -540,7 +536,7 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
             }
             __syncthreads();
         }
-        ds = wave_prefix(ds);
+        const float ds = wave_prefix(of_lane<Mid>(inners, r, g));
         if (lane == 63) through[w] = ds;
 
         // X, Y and the pairs' part of dg
