@@ -352,19 +352,20 @@ struct GradientArgs {
     const T *q, *k, *g, *beta, *d_out;
     T *dq, *dk, *dg, *dbeta;
     const unsigned char *states, *adjoints, *wrong, *r;  // fragments, see gd::Tile
-    const unsigned char *key_ws;
 };
 
-// the tokens 16 w + 4g .. + 3 of channel r in a transposed fragment in LDS
-__device__ __forceinline__ f32x4 four_tokens(const Whole &, const unsigned char *lds, int block, int w, int r, int g)
+// the tokens 16 w + 4g .. + 3 of channel paired(tile, r) of rows in LDS
+template <int DK>
+__device__ __forceinline__ f32x4 four_tokens(const Whole &, const unsigned char *lds, int tile, int w, int r, int g)
 {
-    const int lane = r + 16 * (2 * (w & 1) + (g >> 1));
-    return unpack4(*reinterpret_cast<const uint2 *>(lds + block * 1024 + 16 * lane + 8 * (g & 1)));
+    const uint16_t *q = reinterpret_cast<const uint16_t *>(lds) + (16 * w + 4 * g + (r >> 2)) * KeyTile<bf16_t, DK>::pitch + paired(tile, 4 * (r & 3));
+    return unpack4(__builtin_bit_cast(uint2, lds_read_tr(q)));
 }
-__device__ __forceinline__ f32x4 four_tokens(const Full &, const unsigned char *lds, int block, int w, int r, int g)
+template <int DK>
+__device__ __forceinline__ f32x4 four_tokens(const Full &, const unsigned char *lds, int tile, int w, int r, int g)
 {
-    const int lane = r + 16 * (2 * (w & 1) + (g >> 1));
-    return *reinterpret_cast<const f32x4 *>(lds + block * 2048 + 1024 * (g & 1) + 16 * lane);
+    const float *q = reinterpret_cast<const float *>(lds) + (16 * w + 4 * g) * KeyTile<float, DK>::pitch + paired(tile, r);
+    return f32x4{q[0], q[KeyTile<float, DK>::pitch], q[2 * KeyTile<float, DK>::pitch], q[3 * KeyTile<float, DK>::pitch]};
 }
 
 __device__ __forceinline__ void lds_element(bf16_t *p, float x) { p->bits = uint16_t(pack2(x, x)); }
@@ -397,25 +398,23 @@ __device__ __forceinline__ float of_lane(const f32x4 &acc, int r, int g)
     return (r >> 2) == g ? x : 0.f;
 }
 
-// One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  What more than one wave needs -- rows of k, K^T and Q^T, e,
-// the rows of S and D -- each requests a quarter of and all read from LDS; every request of a turn stands before its first wait: one trip to memory
-// a turn.  The contractions over value columns take kSlice of them at a time.  Bound by the instructions of two waves a SIMD (64 x 64, bf16: 1350 vector and 168
-// matrix ones each): workgroups that go on to another chunk with its requests under way take 90 us where these take 81.
+// One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  What more than one wave needs -- rows of k and q, e, the rows
+// of S and D -- each requests a quarter of and all read from LDS; every request of a turn stands before its first wait: one trip to memory
+// a turn.  The contractions over value columns take kSlice of them at a time.  Bound by the phases of two waves a SIMD (64 x 64, bf16: 1200 vector and 180 matrix
+// instructions each, ten phases between barriers): workgroups that go on to another chunk with its requests under way take 90 us where these take 80.
 // kOne: the values are one slice; two workgroups then fit a compute unit's registers (without it the accumulators are live across the
 // requests of the next slice, and what spills costs more than the second workgroup brings).  kSingle: no other value head shares the keys; without the
-// loop nothing spills (8 x 6 heads of 4096 tokens 81 us, 106 with it; 8 x 16 heads on 8 key heads, 2048 tokens, need it: 112 us with two workgroups a
-// compute unit and 17 registers spilled, 157 with one and none).
+// loop its registers are 173 instead of 243 (8 x 6 heads of 4096 tokens 80 us, 106 with it).
 template <typename T, int DK, bool kOne, bool kSingle>
 __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) void gd_gradients(GradientArgs<T> a)
 {
     using In = typename operands<T, 2>::In;
     using Mid = typename operands<T, 2>::Mid;
-    using Kw = KeyWs<T, DK, true>;
     constexpr int kKs = DK / 32, kCt = DK / 16, kSlice = DK <= 64 ? 64 : 32, kVs = kSlice / 32;
     constexpr int kStates = 2 * kCt * kVs * int(frag_bytes<Mid>), kTiles = 2 * kC * kPitch * 4, kOwn = (kCt * kVs + 3) / 4;
     extern __shared__ __align__(16) unsigned char shared[];  // the rows of S and D, afterwards X and Y; then what is below
-    unsigned char *wrong = shared + (kStates > kTiles ? kStates : kTiles), *key_rows = wrong + 4 * kVs * frag_bytes<Mid>,
-                  *key_columns = key_rows + 4 * kKs * frag_bytes<In>;
+    unsigned char *wrong = shared + (kStates > kTiles ? kStates : kTiles), *keys = wrong + 4 * kVs * frag_bytes<Mid>,
+                  *queries = keys + KeyTile<T, DK>::bytes;
     __shared__ double sum[4][kC];
     __shared__ float bet[4][kC], enters[kC], leaves[kC], pairs[4][kC], through[4];
     float *X = reinterpret_cast<float *>(shared), *Y = X + kC * kPitch;
@@ -427,7 +426,6 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
     const int chunk = int(unit - key_slab * unsigned(s.chunks));
     const int b = int(key_slab / unsigned(s.Hk)), hk = int(key_slab - unsigned(b) * unsigned(s.Hk)), share = s.H / s.Hk;
     const unsigned key_pitch = pitch_of<T>(s, s.Hk, s.dk), value_pitch = pitch_of<T>(s, s.H, s.dv);
-    const Rsrc kw = whole(a.key_ws + size_t(unit) * Kw::bytes);
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     const int blocks = value_blocks(s.dv);
     const size_t state_bytes = emitted_bytes<T>(kCt, s.dv), token_bytes = emitted_bytes<T>(4, s.dv);
@@ -463,7 +461,7 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
     };
 
     f32x4 dq[kCt], dk[kCt];
-    In fq[kKs], fk[kKs], fkc[Kw::blocks / 2];
+    In fq[kKs], fk[kKs];  // the wave's rows
     {
         const Rsrc qr = chunk_rows(a.q, s, b, hk, s.Hk, s.dk, chunk), kr = chunk_rows(a.k, s, b, hk, s.Hk, s.dk, chunk);
         request_gates(hk * share);
@@ -473,16 +471,15 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
             load_row(fq[ks], qr, at);
             load_row(fk[ks], kr, at);
         }
-#pragma unroll
-        for (int o = 0; o < Kw::blocks / 2; ++o) fkc[o] = get<In>(kw, 0, 4 * o + w, lane);  // K^T, then Q^T
         request_slice(hk * share, 0);
         requests_stay();
     }
     put_gates();
 #pragma unroll
-    for (int ks = 0; ks < kKs; ++ks) lds_put(key_rows, w * kKs + ks, lane, fk[ks]);
-#pragma unroll
-    for (int o = 0; o < Kw::blocks / 2; ++o) lds_put(key_columns, 4 * o + w, lane, fkc[o]);
+    for (int ks = 0; ks < kKs; ++ks) {
+        key_put<T, DK>(keys, 16 * w + r, ks, g, fk[ks]);
+        key_put<T, DK>(queries, 16 * w + r, ks, g, fq[ks]);
+    }
 #pragma unroll
     for (int ct = 0; ct < kCt; ++ct) dq[ct] = dk[ct] = zero;
 
@@ -546,9 +543,11 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
             store_element<T>(chunk_rows(a.dbeta, s, b, h, s.H, 1, chunk), (r >> 2) == g ? unsigned(token_at(s, 16 * w + r)) * pitch_of<T>(s, s.H, 1) : kNowhere, db);
         }
         float carry[4] = {0.f, 0.f, 0.f, 0.f};
-        In own[kKs];  // the wave's rows of k
 #pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) own[ks] = lds_get<In>(key_rows, w * kKs + ks, lane);
+        for (int ks = 0; ks < kKs; ++ks) {
+            key_get<T, DK>(fk[ks], keys, 16 * w + r, ks, g);
+            key_get<T, DK>(fq[ks], queries, 16 * w + r, ks, g);
+        }
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             float column = 0.f;
@@ -557,9 +556,10 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
             requests_stay();
 #pragma unroll
             for (int ks = 0; ks < kKs; ++ks) {
-                const In f = lds_get<In>(key_rows, n * kKs + ks, lane);
+                In f;
+                key_get<T, DK>(f, keys, 16 * n + r, ks, g);
                 mma(qk, fq[ks], f);
-                mma(kk, own[ks], f);
+                mma(kk, fk[ks], f);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -592,8 +592,7 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
 #pragma unroll
         for (int ct = 0; ct < kCt; ++ct) {
             if (ct % 2 == 0) requests_stay();
-            const f32x4 qe = four_tokens(In{}, key_columns, Kw::blocks + 2 * ct + (w >> 1), w, r, g);
-            const f32x4 ke = four_tokens(In{}, key_columns, 2 * ct + (w >> 1), w, r, g);
+            const f32x4 qe = four_tokens<DK>(In{}, queries, ct, w, r, g), ke = four_tokens<DK>(In{}, keys, ct, w, r, g);
             enter += qe * read[ct] + ke * erase[ct];
             leave += ke * write[ct];
             dq[ct] += read[ct];
@@ -623,7 +622,9 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
 #pragma unroll
             for (int ct = 0; ct < kCt; ++ct) {
                 if (ct % 2 == 0) requests_stay();
-                const In fkt = lds_get<In>(key_columns, 2 * ct + ks, lane), fqt = lds_get<In>(key_columns, Kw::blocks + 2 * ct + ks, lane);
+                In fkt, fqt;
+                key_column<DK>(fkt, keys, ct, ks, r, g);
+                key_column<DK>(fqt, queries, ct, ks, r, g);
                 mma(dq[ct], fx, fkt);
                 mma(dk[ct], ft, fqt);
                 mma(dk[ct], fy, fkt);
@@ -669,7 +670,7 @@ constexpr size_t gradient_lds()
     using In = typename operands<T, 2>::In;
     using Mid = typename operands<T, 2>::Mid;
     constexpr size_t states = 2 * DK / 16 * vs * frag_bytes<Mid>, tiles = 2 * kC * kPitch * 4;
-    return (states > tiles ? states : tiles) + 4 * vs * frag_bytes<Mid> + 4 * DK / 32 * frag_bytes<In> + KeyWs<T, DK, true>::bytes;
+    return (states > tiles ? states : tiles) + 4 * vs * frag_bytes<Mid> + 2 * KeyTile<T, DK>::bytes;
 }
 
 struct Buffers {
@@ -702,7 +703,7 @@ hipError_t launch(const Shape &s, const GradientPointers &p, void *workspace, hi
     const ChainArgs<T> chain = {s, q, k, v, p.initial, nullptr, nullptr, S, e, ws, ws + at.key_ws};
     const AdjointArgs<T> adjoint = {s, k, d_out, p.d_final, static_cast<T *>(p.dv), p.d_initial, D, r, ws, ws + at.key_ws};
     const GradientArgs<T> gradient = {s, q, k, g, beta, d_out, static_cast<T *>(p.dq), static_cast<T *>(p.dk), static_cast<T *>(p.dg),
-                                      static_cast<T *>(p.dbeta), S, D, e, r, ws + at.key_ws};
+                                      static_cast<T *>(p.dbeta), S, D, e, r};
     const LaunchTimer timer(kKernelGatedDeltaBackward, stream);
     gd_prepare<T, DK, N, true><<<slabs * unsigned(s.chunks), 256, 0, stream>>>(prepare);
     gd_both_chains<T, DK, N><<<dim3((slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 2), 128, 0, stream>>>(chain, adjoint);
