@@ -401,11 +401,11 @@ __device__ __forceinline__ float of_lane(const f32x4 &acc, int r, int g)
 // One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  What more than one wave needs -- rows of k and q, e, the rows
 // of S and D -- each requests a quarter of and all read from LDS; every request of a turn stands before its first wait: one trip to memory
 // a turn.  The contractions over value columns take kSlice of them at a time.  Bound by the phases of two waves a SIMD (64 x 64, bf16: 1200 vector and 180 matrix
-// instructions each, ten phases between barriers): workgroups that go on to another chunk with its requests under way take 90 us where these take 80.
+// instructions each, ten phases between barriers): 8 x 6 heads of 4096 tokens take 79 us, and 90 in
+// workgroups that go on to another chunk with its requests under way.
 // kOne: the values are one slice; two workgroups then fit a compute unit's registers (without it the accumulators are live across the
-// requests of the next slice, and what spills costs more than the second workgroup brings).  kSingle: no other value head shares the keys; without the
-// loop its registers are 173 instead of 243 (8 x 6 heads of 4096 tokens 80 us, 106 with it).
-template <typename T, int DK, bool kOne, bool kSingle>
+// requests of the next slice, and what spills costs more than the second workgroup brings).
+template <typename T, int DK, bool kOne>
 __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) void gd_gradients(GradientArgs<T> a)
 {
     using In = typename operands<T, 2>::In;
@@ -483,11 +483,11 @@ __global__ __launch_bounds__(256, kOne && DK <= 64 && sizeof(T) == 2 ? 2 : 1) vo
 #pragma unroll
     for (int ct = 0; ct < kCt; ++ct) dq[ct] = dk[ct] = zero;
 
-    for (int h = hk * share; h < hk * share + (kSingle ? 1 : share); ++h) {
+    for (int h = hk * share; h < (hk + 1) * share; ++h) {
         // (addresses are formed from here on in every turn: formed once for all, they would be more than the registers hold)
-        if (!kSingle) asm volatile("" : "+v"(lane));
+        asm volatile("" : "+v"(lane));
         r = lane & 15, g = lane >> 4;
-        if (!kSingle && h > hk * share) {
+        if (h > hk * share) {
             request_gates(h);
             request_slice(h, 0);
             requests_stay();
@@ -709,12 +709,10 @@ hipError_t launch(const Shape &s, const GradientPointers &p, void *workspace, hi
     gd_both_chains<T, DK, N><<<dim3((slabs + 7) / 8 * 8 * unsigned(s.dv / 16), 2), 128, 0, stream>>>(chain, adjoint);
     const unsigned key_units = unsigned(s.B) * unsigned(s.Hk) * unsigned(s.chunks);
     constexpr size_t lds = gradient_lds<T, DK>();
-    if (s.dv > (DK <= 64 ? 64 : 32))
-        gd_gradients<T, DK, false, false><<<key_units, 256, lds, stream>>>(gradient);
-    else if (s.H > s.Hk)
-        gd_gradients<T, DK, true, false><<<key_units, 256, lds, stream>>>(gradient);
+    if (s.dv <= (DK <= 64 ? 64 : 32))
+        gd_gradients<T, DK, true><<<key_units, 256, lds, stream>>>(gradient);
     else
-        gd_gradients<T, DK, true, true><<<key_units, 256, lds, stream>>>(gradient);
+        gd_gradients<T, DK, false><<<key_units, 256, lds, stream>>>(gradient);
     return hipGetLastError();
 }
 
