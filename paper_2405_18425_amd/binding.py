@@ -589,28 +589,40 @@ def gated_delta_step(q, k, v, g, beta, state, slots=None, out=None):
     q, k: [B,Hk,dk]; v: [B,H,dv]; g, beta: [B,H]; slots: int32 [B], the state of each sequence (distinct; one outside
     [0, n_slots) marks a padded row, whose output is zero), or None (sequence b has state b) -> out [B,H,dv].
     """
-    q, state = _dev(q, "q"), _dev(state, "state")
-    v = _dev(v, "v", like=q)
-    if q.dim() != 3 or v.dim() != 3 or state.dim() != 4:
-        raise VigError(VIG_ERR_SHAPE, "q and v must be 3-dimensional, state 4-dimensional")
-    (B, Hk, dk), (_, H, dv), n_slots = q.shape, v.shape, state.shape[0]
-    dtype, device = q.dtype, q.get_device()
-    if v.shape[0] != B:
-        raise VigError(VIG_ERR_SHAPE, "v must have the leading dimension of q")
-    _as(k, "k", q.shape, q, dtype, device)
-    _as(g, "g", (B, H), q, dtype, device)
-    _as(beta, "beta", (B, H), q, dtype, device)
-    if state.dtype is not torch.float32 or state.get_device() != device or state.shape != (n_slots, H, dk, dv):
+    # (a small call is bound by what the host does for it: one expression first, and what is wrong only where it is false)
+    try:
+        (B, Hk, dk), (_, H, dv), n_slots = q.shape, v.shape, state.shape[0]
+        dtype, device, heads = q.dtype, q.get_device(), (B, H)
+        fits = (device >= 0 and k.shape == q.shape and v.shape[0] == B and g.shape == heads and beta.shape == heads
+                and state.shape == (n_slots, H, dk, dv) and k.dtype is dtype and v.dtype is dtype and g.dtype is dtype
+                and beta.dtype is dtype and state.dtype is torch.float32 and k.get_device() == device
+                and v.get_device() == device and g.get_device() == device and beta.get_device() == device
+                and state.get_device() == device and q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
+                and g.is_contiguous() and beta.is_contiguous() and state.is_contiguous())
+    except (AttributeError, ValueError, IndexError):
+        fits = False
+    if not fits:
+        q, state = _dev(q, "q"), _dev(state, "state")
+        v = _dev(v, "v", like=q)
+        if q.dim() != 3 or v.dim() != 3 or state.dim() != 4:
+            raise VigError(VIG_ERR_SHAPE, "q and v must be 3-dimensional, state 4-dimensional")
+        (B, Hk, dk), (_, H, dv), n_slots = q.shape, v.shape, state.shape[0]
+        if v.shape[0] != B:
+            raise VigError(VIG_ERR_SHAPE, "v must have the leading dimension of q")
+        _dev(k, "k", q.shape, q)
+        _dev(g, "g", (B, H), q)
+        _dev(beta, "beta", (B, H), q)
         _fp32(state, "state", (n_slots, H, dk, dv), q)
+        device = q.get_device()
     if slots is not None:
         _dev(slots, "slots", (B,))
-        if slots.dtype != torch.int32 or slots.device != q.device:
+        if slots.dtype != torch.int32 or slots.get_device() != device:
             raise VigError(VIG_ERR_DTYPE, "slots must be int32, on the device of the other tensors")
     out = torch.empty_like(v) if out is None else _dev(out, "out", v.shape, q)
-    with _here(q.get_device()):
+    with _here(device):
         st = lib().gated_delta_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(),
                                     state.data_ptr(), _ptr(slots), out.data_ptr(), B, H, Hk, dk, dv, n_slots,
-                                    _dtype_code(q), torch._C._cuda_getCurrentRawStream(q.get_device()))
+                                    _dtype_code(q), torch._C._cuda_getCurrentRawStream(device))
     _check(st, "gated_delta_step")
     return out
 
