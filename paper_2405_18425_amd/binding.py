@@ -628,20 +628,31 @@ def gated_delta_step(q, k, v, g, beta, state, slots=None, out=None):
 
 
 def _norm_args(x, groups, weight, bias, act):
+    try:  # (as in gated_delta_step)
+        channels, dtype, device, n = x.shape[-1:], x.dtype, x.get_device(), x.numel()
+        fits = device >= 0 and n > 0 and x.dim() >= 2 and x.is_contiguous()
+        if weight is not None:
+            fits = (fits and weight.shape == channels and bias.shape == channels and weight.dtype is dtype and bias.dtype is dtype
+                    and weight.get_device() == device and bias.get_device() == device and weight.is_contiguous()
+                    and bias.is_contiguous())
+    except (AttributeError, IndexError):
+        fits = False
     if act not in ACTS:
         raise VigError(VIG_ERR_UNSUPPORTED, f"act must be one of {sorted(ACTS)}")
-    x = _dev(x, "x")
-    if x.dim() < 2:
-        raise VigError(VIG_ERR_SHAPE, "x must be [B, ..., C]")
-    B, C = x.shape[0], x.shape[-1]
-    if B == 0 or C == 0 or x.numel() == 0:
-        raise VigError(VIG_ERR_SHAPE, "x has no elements")
     if (weight is None) != (bias is None):
         raise VigError(VIG_ERR_NULL, "weight and bias come together")
-    if weight is not None:
-        _as(weight, "weight", (C,), x, x.dtype, x.get_device())
-        _as(bias, "bias", (C,), x, x.dtype, x.get_device())
-    return (B, x.numel() // (B * C), C, groups), _dtype_code(x), ACTS[act]
+    if not fits:
+        _dev(x, "x")
+        if x.dim() < 2:
+            raise VigError(VIG_ERR_SHAPE, "x must be [B, ..., C]")
+        if x.numel() == 0:
+            raise VigError(VIG_ERR_SHAPE, "x has no elements")
+        if weight is not None:
+            _dev(weight, "weight", x.shape[-1:], x)
+            _dev(bias, "bias", x.shape[-1:], x)
+        n = x.numel()
+    B, C = x.shape[0], x.shape[-1]
+    return (B, n // (B * C), C, groups), _dtype_code(x), ACTS[act]
 
 
 def group_norm_act_fwd(x, groups: int, weight=None, bias=None, eps: float = 1e-5, act="silu", out=None, stats=None,
@@ -652,7 +663,7 @@ def group_norm_act_fwd(x, groups: int, weight=None, bias=None, eps: float = 1e-5
     sizes, code, act_code = _norm_args(x, groups, weight, bias, act)
     out = torch.empty_like(x) if out is None else _dev(out, "out", x.shape, x)
     if stats is None:
-        stats = torch.empty((sizes[0], max(groups, 0), 2), dtype=torch.float32, device=x.device)
+        stats = torch.empty(sizes[0], max(groups, 0), 2, dtype=torch.float32, device=x.device)
     else:
         _fp32(stats, "stats", (sizes[0], groups, 2), x)
     workspace, ws_bytes = _workspace(workspace, _bytes("group_norm_workspace_bytes", *sizes, code), x.device)
