@@ -67,11 +67,13 @@ __device__ __forceinline__ float act_slope(float z)
     return s * fmaf(z, 1.f - s, 1.f);
 }
 
+// the sum over the 64 lanes, in each of them
 __device__ __forceinline__ float wave_sum(float x)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-    return x;
+    x = row_scan<0>(x);
+    x += dpp_or_zero<0x142>(x);  // row_bcast:15
+    x += dpp_or_zero<0x143>(x);  // row_bcast:31, the whole sum in lane 63
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
 struct Plan {
