@@ -474,6 +474,11 @@ def _as(t, name, shape, like, dtype, device: int):
 
 def _fp32(t, name, shape, like):
     """An fp32 tensor (a state, statistics) beside tensors of either dtype."""
+    try:
+        if t.shape == shape and t.dtype is torch.float32 and t.get_device() == like.get_device() and t.is_contiguous():
+            return t  # (as in _as; like is a GPU tensor)
+    except AttributeError:
+        pass
     t = _dev(t, name, shape)
     if t.dtype != torch.float32 or t.device != like.device:
         raise VigError(VIG_ERR_DTYPE, f"{name} must be float32, on the device of the other tensors")
