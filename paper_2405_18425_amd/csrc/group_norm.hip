@@ -76,6 +76,9 @@ __device__ __forceinline__ float wave_sum(float x)
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
+// (a NaN stays one: fmaxf would make a variance of zero of it)
+__device__ __forceinline__ float not_below_zero(float x) { return x < 0.f ? 0.f : x; }
+
 struct Plan {
     int B, L, C, G, strips, rows;  // rows of a strip
     int vecs, row_groups;          // 16-byte pieces of a row; rows that a workgroup takes at a time
@@ -228,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void norm_strip_kernel(NormArgs<T> a)
             const float inv = n > 0 ? 1.f / float(n) : 0.f;
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                entry[rg * p.C + vec * V + e] = make_float2(fmaf(s1[e], inv, base.v[e]), fmaxf(fmaf(-s1[e] * inv, s1[e], s2[e]), 0.f));
+                entry[rg * p.C + vec * V + e] = make_float2(fmaf(s1[e], inv, base.v[e]), not_below_zero(fmaf(-s1[e] * inv, s1[e], s2[e])));
         }
     __syncthreads();
     const int lane = threadIdx.x & 63, width = p.C / p.G;
@@ -250,7 +253,7 @@ __global__ __launch_bounds__(kThreads) void norm_strip_kernel(NormArgs<T> a)
         s2 = wave_sum(s2);
         if (lane == 0) {
             const float all = float(rows) * float(width);
-            a.partial[size_t(blockIdx.x) * p.G + j] = make_float2(mean0 + s1 / all, fmaxf(s2 - s1 * (s1 / all), 0.f));
+            a.partial[size_t(blockIdx.x) * p.G + j] = make_float2(mean0 + s1 / all, not_below_zero(s2 - s1 * (s1 / all)));
         }
     }
 }
@@ -276,7 +279,7 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs<T> a)
         }
         s1 = wave_sum(s1);
         s2 = wave_sum(s2);
-        const float all = float(p.L) * float(width), mean = mean0 + s1 / all, rstd = 1.f / sqrtf(fmaxf(s2 - s1 * (s1 / all), 0.f) / all + a.eps);
+        const float all = float(p.L) * float(width), mean = mean0 + s1 / all, rstd = 1.f / sqrtf(not_below_zero(s2 - s1 * (s1 / all)) / all + a.eps);
         if (lane == 0) {
             stat[j] = make_float2(mean, rstd);
             if (strip == 0) *reinterpret_cast<float2 *>(a.stats + 2 * (size_t(b) * p.G + j)) = make_float2(mean, rstd);
