@@ -12,8 +12,9 @@
 // Measured (bf16): 8 x 4096 x 384 in 6 groups 9.8 + 11.6 us, 25 MB in, 25 MB in again and 25 MB out: 2.6 and 4.3 TB/s; 16 x 3136 x 128 in 2 groups, gradient,
 // 10.3 + 9.5 us; 64 x 49 x 1024 in 16 groups, one launch, 7.0 us for 13 MB, mostly the latency of one trip in, the sums and one trip out.
 //
-// Variances are sums of squared distances, never a difference of large sums: a thread's values are taken relative to the first of
-// them, threads and strips are joined by their means.
+// Variances are sums of terms that are not negative, never a difference: runs of four rows, a strip's channels and threads and the strips are
+// joined by the squared distances of their means from the mean of all, which a pass before has.  (From the first of those means, as one pass would have
+// to, an outlier there is in all terms: with one channel of 8192 at 3.3 and the others 0, 1 / sqrt(var) was off by 1.4 %.)
 #include "vig_common.hpp"
 #include "vig_kernels.hpp"
 #include "vig_timing.hpp"
@@ -76,8 +77,7 @@ __device__ __forceinline__ float wave_sum(float x)
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
-// (a NaN stays one: fmaxf would make a variance of zero of it)
-__device__ __forceinline__ float not_below_zero(float x) { return x < 0.f ? 0.f : x; }
+constexpr int kWorkgroups = 1024;  // of a launch over strips, four a compute unit; no element has more strips
 
 struct Plan {
     int B, L, C, G, strips, rows;  // rows of a strip
@@ -91,7 +91,7 @@ struct NormArgs {
     T *out;
     float *stats;                // [B, G, 2] mean, rstd
     float eps;
-    float2 *partial;             // [B][strips][G] mean, sum of squared distances
+    float2 *partial;             // [B][G][strips] mean, squared distances from it; of the gradient [B][strips][G], sums
     // gradient
     const float *in_stats;
     const T *d_out;
@@ -196,6 +196,18 @@ __device__ __forceinline__ int rows_at(const Plan &p, int strip, int &first)
 }
 __device__ __forceinline__ int rows_of_group(int rows, int group, int groups) { return group < rows ? (rows - group + groups - 1) / groups : 0; }
 
+// Rows that a thread takes at a time for its channels' means and squared distances
+constexpr int kRun = 4;
+
+// Of n values with mean v.x and squared distances v.y from it: what they add to the squared distances from `mean`, which is next to the whole's
+// mean, and to what it is off by.  (Off by a few roundings, `mean` adds their square to a variance: nothing.)
+__device__ __forceinline__ void join(float2 v, float n, float mean, float &rest, float &sq)
+{
+    const float d = v.x - mean;
+    rest = fmaf(n, d, rest);
+    sq += fmaf(n * d, d, v.y);
+}
+
 // Mean and squared distances of every group over the rows of a strip
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_strip_kernel(NormArgs<T> a)
@@ -211,51 +223,102 @@ __global__ __launch_bounds__(kThreads) void norm_strip_kernel(NormArgs<T> a)
     if (rg < p.row_groups)
         for (int vec = p.row_groups > 1 ? int(threadIdx.x) - rg * p.vecs : int(threadIdx.x); vec < p.vecs; vec += kThreads) {
             const int n = rows_of_group(rows, rg, p.row_groups);
-            float s1[V], s2[V];
-            Values<T> base, y;
-#pragma unroll
-            for (int e = 0; e < V; ++e) s1[e] = s2[e] = base.v[e] = 0.f;
+            // Of distances from the first row: of a channel far from zero they keep their bits.  Runs of kRun rows; the first one, from the first row on, has
+            // what is left (rows that it does not have are read as its last one, and count nothing).
+            float mean[V], sq[V];
+            Values<T> base, y[kRun];
             const T *q = x + size_t(rg) * p.C + vec * V;
             const size_t step = size_t(p.row_groups) * p.C;
-            if (n > 0) load(base, q);
-#pragma unroll 4
-            for (int i = 1; i < n; ++i) {
-                load(y, q + i * step);
+            const int head = n > 0 ? (n - 1) % kRun + 1 : 0;
+#pragma unroll
+            for (int e = 0; e < V; ++e) mean[e] = sq[e] = base.v[e] = 0.f;
+            if (n > 0) {
+                load(base, q);
+#pragma unroll
+                for (int o = 1; o < kRun; ++o) load(y[o], q + (o < head ? o : head - 1) * step);
+                const float inv = 1.f / float(head);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float d = y.v[e] - base.v[e];
-                    s1[e] += d;
-                    s2[e] = fmaf(d, d, s2[e]);
+                    float sum = 0.f;
+#pragma unroll
+                    for (int o = 1; o < kRun; ++o) sum += y[o].v[e] = o < head ? y[o].v[e] - base.v[e] : 0.f;
+                    mean[e] = sum * inv;
+                    sq[e] = mean[e] * mean[e];
+#pragma unroll
+                    for (int o = 1; o < kRun; ++o) {
+                        const float d = o < head ? y[o].v[e] - mean[e] : 0.f;
+                        sq[e] = fmaf(d, d, sq[e]);
+                    }
                 }
             }
-            const float inv = n > 0 ? 1.f / float(n) : 0.f;
+            for (int i = head; i < n; i += kRun) {
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                entry[rg * p.C + vec * V + e] = make_float2(fmaf(s1[e], inv, base.v[e]), not_below_zero(fmaf(-s1[e] * inv, s1[e], s2[e])));
+                for (int o = 0; o < kRun; ++o) load(y[o], q + (i + o) * step);
+                const float share = float(kRun) / float(i + kRun), weight = float(i) * share;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    float sum = 0.f, own = 0.f;
+#pragma unroll
+                    for (int o = 0; o < kRun; ++o) sum += y[o].v[e] -= base.v[e];
+                    const float run = sum * (1.f / kRun), d = run - mean[e];
+#pragma unroll
+                    for (int o = 0; o < kRun; ++o) own = fmaf(y[o].v[e] - run, y[o].v[e] - run, own);
+                    sq[e] += fmaf(weight * d, d, own);
+                    mean[e] = fmaf(share, d, mean[e]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) entry[rg * p.C + vec * V + e] = make_float2(base.v[e] + mean[e], sq[e]);
         }
     __syncthreads();
     const int lane = threadIdx.x & 63, width = p.C / p.G;
+    const int least = rows / p.row_groups, more = rows - least * p.row_groups, there = least > 0 ? p.row_groups : more;  // (rows of a row group, see rows_of_group)
     for (int j = threadIdx.x >> 6; j < p.G; j += kThreads / 64) {
         const float2 *own = entry + j * width;
-        const float mean0 = own[0].x;  // distances from one of the means: sums of them lose nothing
-        float s1 = 0.f, s2 = 0.f;
-        for (int g = 0; g < p.row_groups; ++g) {
-            const float n = float(rows_of_group(rows, g, p.row_groups));
-            if (n > 0.f)
-                for (int c = lane; c < width; c += 64) {
-                    const float2 v = own[g * p.C + c];
-                    const float d = v.x - mean0;
-                    s1 = fmaf(n, d, s1);
-                    s2 += fmaf(n * d, d, v.y);
-                }
-        }
-        s1 = wave_sum(s1);
-        s2 = wave_sum(s2);
-        if (lane == 0) {
-            const float all = float(rows) * float(width);
-            a.partial[size_t(blockIdx.x) * p.G + j] = make_float2(mean0 + s1 / all, not_below_zero(s2 - s1 * (s1 / all)));
-        }
+        const auto entries = [&](auto take) {
+            for (int g = 0; g < there; ++g) {
+                const float n = float(g < more ? least + 1 : least);
+                for (int c = lane; c < width; c += 64) take(n, own[g * p.C + c]);
+            }
+        };
+        const float inv = 1.f / (float(rows) * float(width)), first = own[0].x;
+        float s = 0.f, rest = 0.f, sq = 0.f;
+        entries([&](float n, float2 v) { s = fmaf(n, v.x - first, s); });
+        const float mean = fmaf(wave_sum(s), inv, first);
+        entries([&](float n, float2 v) { join(v, n, mean, rest, sq); });
+        rest = wave_sum(rest);
+        sq = wave_sum(sq);
+        if (lane == 0) a.partial[(size_t(b) * p.G + j) * p.strips + strip] = make_float2(fmaf(rest, inv, mean), sq);
     }
+}
+
+// Mean and variance of a group from its strips' means and squared distances, in every lane.  The pairs are read once, all requests on their way together.
+template <int kMine /* pairs of a lane */>
+__device__ __forceinline__ float2 join_strips(const Plan &p, const float2 *part, int lane, int width)
+{
+    asm volatile("" : "+v"(lane));  // (what depends on the lane is formed here, not ahead of the loop over groups for every form of this)
+    float2 v[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int at = 64 * i + lane;
+        v[i] = part[at < p.strips ? at : 0];
+    }
+    const float inv = 1.f / (float(p.L) * float(width)), whole = float(p.rows) * float(width),
+                last = float(p.L - (p.strips - 1) * p.rows) * float(width), first = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v[0].x)));
+    const auto values = [&](int i) {
+        const int left = p.strips - 1 - (64 * i + lane);
+        return left > 0 ? whole : left == 0 ? last : 0.f;
+    };
+    float s = 0.f, rest = 0.f, sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        if (64 * i + lane >= p.strips) v[i].y = 0.f;
+        s = fmaf(values(i), v[i].x - first, s);
+    }
+    const float mean = fmaf(wave_sum(s), inv, first);
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) join(v[i], values(i), mean, rest, sq);
+    return make_float2(fmaf(wave_sum(rest), inv, mean), wave_sum(sq) * inv);
 }
 
 template <typename T, bool kSilu>
@@ -267,19 +330,10 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs<T> a)
     const unsigned b = blockIdx.x / unsigned(p.strips), strip = blockIdx.x - b * unsigned(p.strips);
     const int lane = threadIdx.x & 63, width = p.C / p.G;
     for (int j = threadIdx.x >> 6; j < p.G; j += kThreads / 64) {  // the strips' sums of the element
-        const float2 *part = a.partial + size_t(b) * p.strips * p.G + j;
-        const float mean0 = part[0].x;  // distances from one of the means: sums of them lose nothing
-        int first;
-        float s1 = 0.f, s2 = 0.f;
-        for (int i = lane; i < p.strips; i += 64) {
-            const float2 v = part[size_t(i) * p.G];
-            const float d = v.x - mean0, n = float(rows_at(p, i, first)) * float(width);
-            s1 = fmaf(n, d, s1);
-            s2 += fmaf(n * d, d, v.y);
-        }
-        s1 = wave_sum(s1);
-        s2 = wave_sum(s2);
-        const float all = float(p.L) * float(width), mean = mean0 + s1 / all, rstd = 1.f / sqrtf(not_below_zero(s2 - s1 * (s1 / all)) / all + a.eps);
+        const float2 *part = a.partial + (size_t(b) * p.G + j) * p.strips;
+        const float2 s = p.strips <= 64 ? join_strips<1>(p, part, lane, width) : p.strips <= 256 ? join_strips<4>(p, part, lane, width)
+                                                                                              : join_strips<kWorkgroups / 64>(p, part, lane, width);
+        const float mean = s.x, rstd = 1.f / sqrtf(s.y + a.eps);
         if (lane == 0) {
             stat[j] = make_float2(mean, rstd);
             if (strip == 0) *reinterpret_cast<float2 *>(a.stats + 2 * (size_t(b) * p.G + j)) = make_float2(mean, rstd);
@@ -456,8 +510,6 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormArgs<T> a, unsi
 }
 
 // ---- plans -----------------------------------------------------------------------------------------
-
-constexpr int kWorkgroups = 1024;  // four a compute unit
 
 Plan plan_of(int B, int L, int C, int G, int vec)
 {

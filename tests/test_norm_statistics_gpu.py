@@ -1,11 +1,30 @@
-"""GPU tests of the channels-last group norm's statistics: values that are not finite."""
+"""GPU tests of the channels-last group norm's statistics: values that are not finite or overflow, groups whose channels, rows or strips
+have means of their own.
+
+Tolerances: a variance is a sum of terms that are not negative, so it is off by at most as many half steps (2^-24) as additions follow one another
+(259 of a thread, 9 + 6 of a workgroup's entries and lanes, 16 + 6 of strips and lanes) and a term has roundings: under 2^-15, and half of that for
+1 / sqrt.  A mean is off by 2^-16 of the spread (its sum's terms are distances) and two roundings of its own."""
 import pytest
 import torch
+
+import delta_norm_ref as ref
 
 pytestmark = pytest.mark.gpu
 
 BF16, F32 = torch.bfloat16, torch.float32
 INF = float("inf")
+
+
+def _stats_close(stats, x, groups, what):
+    """stats against 64 bits."""
+    _, want = ref.norm_fwd(x, groups, act="none")
+    got = stats.detach().cpu().double()
+    std = (1 / want[..., 1] ** 2 - 1e-5).clamp_min(0).sqrt()
+    worst_r = ((got[..., 1] - want[..., 1]).abs() / want[..., 1]).max().item() * 2 ** 16
+    worst_m = ((got[..., 0] - want[..., 0]).abs() / (2 ** -16 * std + 2 ** -23 * want[..., 0].abs() + 1e-30)).max().item()
+    assert worst_r <= 1.0, f"{what}: 1 / sqrt(var) {worst_r:.2f} of the bound"
+    assert worst_m <= 1.0, f"{what}: mean {worst_m:.2f} of the bound"
+    return want
 
 
 # 40 tokens: a group in one workgroup's registers, one launch; 3000: partial sums of strips, two launches
@@ -35,3 +54,73 @@ def test_values_that_are_not_finite_reach_their_group_only(dtype, L, bad, at):
     assert torch.equal(stats.flatten(0, 1)[[i for i in range(12) if i != 5]], clean_stats.flatten(0, 1)[[i for i in range(12) if i != 5]])
     assert torch.equal(dx.transpose(1, 2)[others], clean_grads[0].transpose(1, 2)[others])
     assert torch.equal(dw[rest], clean_grads[1][rest]) and torch.equal(db, clean_grads[2])
+
+
+@pytest.mark.parametrize("dtype", (BF16, F32))
+@pytest.mark.parametrize("L", (40, 3000))
+def test_squares_that_overflow(dtype, L):
+    """Values around 1e20: the variance is infinite in 32 bits, 1 / sqrt of it 0 and the output the bias, in both forms."""
+    from paper_2405_18425_amd import binding as vb
+
+    gen = torch.Generator().manual_seed(L)
+    x = torch.randn(2, L, 64, generator=gen)
+    x[1, :, 16:32] *= 1e20
+    x = x.to(dtype).cuda()
+    b = torch.randn(64, generator=gen).to(dtype).cuda()
+    y, stats = vb.group_norm_act_fwd(x, 4, torch.ones_like(b), b, act="none")
+    assert stats[1, 1, 1] == 0 and torch.isfinite(stats).all()
+    assert torch.equal(y[1, :, 16:32], b[16:32].expand(L, 16))
+    want = ref.norm_fwd(x, 4)[1]
+    assert abs(stats[1, 1, 0].item() - want[1, 1, 0].item()) <= 2 ** -16 * 1e20
+
+
+@pytest.mark.parametrize("spread", (0.0, 0.01, 1.0))
+@pytest.mark.parametrize("value", (3.3, 37.7, 1000.3))
+@pytest.mark.parametrize("dtype,B,L,C,groups", ((BF16, 2, 33, 8192, 1), (F32, 2, 33, 8192, 1), (F32, 1, 260, 4096, 1), (BF16, 2, 500, 2048, 2),
+                                                (F32, 3, 1700, 24, 1)))
+def test_first_channel_of_a_group_apart(dtype, B, L, C, groups, value, spread):
+    from paper_2405_18425_amd import binding as vb
+
+    gen = torch.Generator().manual_seed(C)
+    x = torch.randn(B, L, C, generator=gen) * spread
+    x[:, :, ::C // groups] += value
+    x = x.to(dtype).cuda()
+    _stats_close(vb.group_norm_act_fwd(x, groups)[1], x, groups, f"{dtype} {B}x{L}x{C}/{groups} {value} {spread}")
+
+
+@pytest.mark.parametrize("value", (3.3, 1000.3))
+@pytest.mark.parametrize("spread", (0.0, 0.01))
+def test_first_strip_apart(value, spread):
+    """16384 rows of one element are 1024 strips."""
+    from paper_2405_18425_amd import binding as vb
+
+    gen = torch.Generator().manual_seed(1)
+    x = torch.randn(1, 16384, 1024, generator=gen) * spread
+    x[:, :16] += value
+    x = x.cuda()
+    _stats_close(vb.group_norm_act_fwd(x, 1)[1], x, 1, f"{value} {spread}")
+
+
+@pytest.mark.parametrize("value", (3.3, 1000.3))
+def test_first_row_apart(value):
+    """1024 elements are a strip each, a thread goes over all 1024 rows: a first token before padding with zeros."""
+    from paper_2405_18425_amd import binding as vb
+
+    x = torch.zeros(1024, 1024, 520, device="cuda")
+    x[:, 0] = value
+    stats = vb.group_norm_act_fwd(x, 1)[1]
+    assert torch.equal(stats, stats[:1].expand_as(stats))
+    _stats_close(stats[:1], x[:1], 1, f"{value}")
+
+
+@pytest.mark.parametrize("L", (40, 3000))
+def test_mean_far_from_zero(L):
+    """Values around 1000 with a spread of 1: a mean is a number of 32 bits, so an output is off by two of its roundings, 2^-23 of 1000 in units of the spread."""
+    from paper_2405_18425_amd import binding as vb
+
+    gen = torch.Generator().manual_seed(L)
+    x = (1000 + torch.randn(2, L, 64, generator=gen)).cuda()
+    y, stats = vb.group_norm_act_fwd(x, 4, act="none")
+    _stats_close(stats, x, 4, f"{L}")
+    want = ref.norm_fwd(x, 4, act="none")[0]
+    assert ((y.cpu().double() - want).abs() <= 1001 * 2 ** -23 + 2 ** -15 * want.abs()).all()
