@@ -129,6 +129,20 @@ __device__ __forceinline__ void by_group(const float2 *pair, int c, int width, f
     }
 }
 
+// a power of two of values, two by two
+template <int N>
+__device__ __forceinline__ float sum_of(const float (&x)[N])
+{
+    float s[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = x[i];
+#pragma unroll
+    for (int n = N / 2; n > 0; n /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i) s[i] += s[i + n];
+    return s[0];
+}
+
 // ---- a group per workgroup -------------------------------------------------------------------------
 
 template <typename T, int R /* pieces of a thread */, bool kSilu>
@@ -141,8 +155,10 @@ __global__ __launch_bounds__(kThreads) void norm_group_kernel(NormArgs<T> a)
     const int width = p.C / p.G, pieces = width / V, all = p.L * pieces;
     const size_t base = size_t(b) * p.L * p.C + size_t(j) * width;
     const int w = threadIdx.x >> 6;
+    // Distances from the group's first value, then from their mean: of values that are next to each other they keep their bits, and of values that are
+    // all the same nothing is left.  Where the first value is an outlier, their sums, joined two by two, are off by a rounding or two of it.
+    const float first = io<T>::load(a.x + base);
     Values<T> x[R];
-    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int at = int(threadIdx.x) + i * kThreads, row = at / pieces, c = (at - row * pieces) * V;
@@ -150,15 +166,19 @@ __global__ __launch_bounds__(kThreads) void norm_group_kernel(NormArgs<T> a)
             load(x[i], a.x + base + size_t(row) * p.C + c);
         else
 #pragma unroll
-            for (int e = 0; e < V; ++e) x[i].v[e] = 0.f;
-#pragma unroll
-        for (int e = 0; e < V; ++e) sum += x[i].v[e];
+            for (int e = 0; e < V; ++e) x[i].v[e] = first;
     }
-    const float n = float(p.L) * float(width);
-    sum = wave_sum(sum);
+    float sums[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[i].v[e] -= first;
+        sums[i] = sum_of(x[i].v);
+    }
+    const float sum = wave_sum(sum_of(sums)), inv = 1.f / (float(p.L) * float(width));
     if ((threadIdx.x & 63) == 0) part[0][w] = sum;
     __syncthreads();
-    const float mean = ((part[0][0] + part[0][1]) + (part[0][2] + part[0][3])) / n;
+    const float mean = ((part[0][0] + part[0][1]) + (part[0][2] + part[0][3])) * inv;
     float sq = 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -172,8 +192,8 @@ __global__ __launch_bounds__(kThreads) void norm_group_kernel(NormArgs<T> a)
     sq = wave_sum(sq);
     if ((threadIdx.x & 63) == 0) part[1][w] = sq;
     __syncthreads();
-    const float var = ((part[1][0] + part[1][1]) + (part[1][2] + part[1][3])) / n, rstd = 1.f / sqrtf(var + a.eps);
-    if (threadIdx.x == 0) *reinterpret_cast<float2 *>(a.stats + 2 * size_t(blockIdx.x)) = make_float2(mean, rstd);
+    const float var = ((part[1][0] + part[1][1]) + (part[1][2] + part[1][3])) * inv, rstd = 1.f / sqrtf(var + a.eps);
+    if (threadIdx.x == 0) *reinterpret_cast<float2 *>(a.stats + 2 * size_t(blockIdx.x)) = make_float2(first + mean, rstd);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int at = int(threadIdx.x) + i * kThreads, row = at / pieces, c = (at - row * pieces) * V;

@@ -1,5 +1,5 @@
 """GPU tests of the channels-last group norm's statistics: values that are not finite or overflow, groups whose channels, rows or strips
-have means of their own.
+have means of their own, constant groups.
 
 Tolerances: a variance is a sum of terms that are not negative, so it is off by at most as many half steps (2^-24) as additions follow one another
 (259 of a thread, 9 + 6 of a workgroup's entries and lanes, 16 + 6 of strips and lanes) and a term has roundings: under 2^-15, and half of that for
@@ -124,3 +124,33 @@ def test_mean_far_from_zero(L):
     _stats_close(stats, x, 4, f"{L}")
     want = ref.norm_fwd(x, 4, act="none")[0]
     assert ((y.cpu().double() - want).abs() <= 1001 * 2 ** -23 + 2 ** -15 * want.abs()).all()
+
+
+# (values of a group: 8192 and 16384 are the most of one workgroup in fp32 and bf16)
+@pytest.mark.parametrize("value", (3.3, 37.7, 1000.3, 100000.3, -0.1))
+@pytest.mark.parametrize("dtype,L,C,groups", ((F32, 512, 64, 4), (BF16, 1024, 64, 4), (F32, 33, 64, 4), (F32, 512, 520, 65), (F32, 3000, 64, 4), (BF16, 3000, 2048, 1)))
+def test_constant_groups_are_the_bias(dtype, L, C, groups, value):
+    from paper_2405_18425_amd import binding as vb
+
+    x = torch.full((2, L, C), value, device="cuda").to(dtype)
+    w, b = torch.linspace(0.5, 1.5, C).to(dtype).cuda(), torch.linspace(-1, 1, C).to(dtype).cuda()
+    y, stats = vb.group_norm_act_fwd(x, groups, w, b, act="none")
+    assert torch.equal(y, b.expand_as(y))
+    assert (stats[..., 0] == x[0, 0, 0].float()).all()
+    assert ((stats[..., 1].double() - 1e-5 ** -0.5).abs() <= 2 ** -22 * 1e-5 ** -0.5).all()  # (of a 32-bit eps, a root and a quotient)
+
+
+@pytest.mark.parametrize("value", (0.0, 37.7, 1000.3))
+@pytest.mark.parametrize("first", (0.0, 500.0))
+def test_largest_group_of_one_workgroup(value, first):
+    """8192 values: the mean within 2^-16 of the spread and two of its own roundings, also where the first value is an outlier."""
+    from paper_2405_18425_amd import binding as vb
+
+    gen = torch.Generator().manual_seed(3)
+    x = value + torch.randn(2, 512, 64, generator=gen)
+    x[:, 0, ::16] += first
+    x = x.cuda()
+    y, stats = vb.group_norm_act_fwd(x, 4, act="none")
+    _stats_close(stats, x, 4, f"{value} {first}")
+    want = ref.norm_fwd(x, 4, act="none")[0]
+    assert ((y.cpu().double() - want).abs() <= (abs(value) + 1) * 2 ** -23 + 2 ** -15 * (1 + want.abs())).all()
