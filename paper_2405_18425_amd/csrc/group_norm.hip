@@ -91,6 +91,7 @@ struct NormArgs {
     T *out;
     float *stats;                // [B, G, 2] mean, rstd
     float eps;
+    unsigned first_block;        // of the launch
     float2 *partial;             // [B][G][strips] mean, squared distances from it; of the gradient [B][strips][G], sums
     // gradient
     const float *in_stats;
@@ -151,7 +152,7 @@ __global__ __launch_bounds__(kThreads) void norm_group_kernel(NormArgs<T> a)
     constexpr int V = kVec<T>, kWaves = kThreads / 64;
     __shared__ float part[2][kWaves];
     const Plan &p = a.p;
-    const unsigned b = blockIdx.x / unsigned(p.G), j = blockIdx.x - b * unsigned(p.G);
+    const unsigned block = a.first_block + blockIdx.x, b = block / unsigned(p.G), j = block - b * unsigned(p.G);
     const int width = p.C / p.G, pieces = width / V, all = p.L * pieces;
     const size_t base = size_t(b) * p.L * p.C + size_t(j) * width;
     const int w = threadIdx.x >> 6;
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(kThreads) void norm_group_kernel(NormArgs<T> a)
     if ((threadIdx.x & 63) == 0) part[1][w] = sq;
     __syncthreads();
     const float var = ((part[1][0] + part[1][1]) + (part[1][2] + part[1][3])) * inv, rstd = 1.f / sqrtf(var + a.eps);
-    if (threadIdx.x == 0) *reinterpret_cast<float2 *>(a.stats + 2 * size_t(blockIdx.x)) = make_float2(first + mean, rstd);
+    if (threadIdx.x == 0) *reinterpret_cast<float2 *>(a.stats + 2 * size_t(block)) = make_float2(first + mean, rstd);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int at = int(threadIdx.x) + i * kThreads, row = at / pieces, c = (at - row * pieces) * V;
@@ -235,7 +236,7 @@ __global__ __launch_bounds__(kThreads) void norm_strip_kernel(NormArgs<T> a)
     constexpr int V = kVec<T>;
     extern __shared__ __align__(16) float2 entry[];  // [row_groups][C] mean, squared distances
     const Plan &p = a.p;
-    const unsigned b = blockIdx.x / unsigned(p.strips), strip = blockIdx.x - b * unsigned(p.strips);
+    const unsigned block = a.first_block + blockIdx.x, b = block / unsigned(p.strips), strip = block - b * unsigned(p.strips);
     int first;
     const int rows = rows_at(p, int(strip), first);
     const T *x = a.x + (size_t(b) * p.L + first) * p.C;
@@ -347,7 +348,7 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs<T> a)
     constexpr int V = kVec<T>;
     extern __shared__ __align__(16) float2 stat[];  // [G] mean, rstd
     const Plan &p = a.p;
-    const unsigned b = blockIdx.x / unsigned(p.strips), strip = blockIdx.x - b * unsigned(p.strips);
+    const unsigned block = a.first_block + blockIdx.x, b = block / unsigned(p.strips), strip = block - b * unsigned(p.strips);
     const int lane = threadIdx.x & 63, width = p.C / p.G;
     for (int j = threadIdx.x >> 6; j < p.G; j += kThreads / 64) {  // the strips' sums of the element
         const float2 *part = a.partial + (size_t(b) * p.G + j) * p.strips;
@@ -413,7 +414,7 @@ __global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormArgs<T> a)
     constexpr int V = kVec<T>;
     extern __shared__ __align__(16) float2 entry[];  // [row_groups][C]
     const Plan &p = a.p;
-    const unsigned b = blockIdx.x / unsigned(p.strips), strip = blockIdx.x - b * unsigned(p.strips);
+    const unsigned block = a.first_block + blockIdx.x, b = block / unsigned(p.strips), strip = block - b * unsigned(p.strips);
     int first;
     const int rows = rows_at(p, int(strip), first);
     const size_t at = (size_t(b) * p.L + first) * p.C;
@@ -445,7 +446,7 @@ __global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormArgs<T> a)
     for (int c = threadIdx.x; c < p.C; c += kThreads) {
         float2 s = entry[c];
         for (int g = 1; g < p.row_groups; ++g) s.x += entry[g * p.C + c].x, s.y += entry[g * p.C + c].y;
-        a.channel[size_t(blockIdx.x) * p.C + c] = s;
+        a.channel[size_t(block) * p.C + c] = s;
         const float w = a.weight ? io<T>::load(a.weight + c) : 1.f;
         entry[c] = make_float2(s.x * w, s.y * w);  // (a thread's own channel: no other reads it before the barrier)
     }
@@ -456,7 +457,7 @@ __global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormArgs<T> a)
         for (int c = lane; c < width; c += 64) s1 += entry[j * width + c].x, s2 += entry[j * width + c].y;
         s1 = wave_sum(s1);
         s2 = wave_sum(s2);
-        if (lane == 0) a.partial[size_t(blockIdx.x) * p.G + j] = make_float2(s1, s2);
+        if (lane == 0) a.partial[size_t(block) * p.G + j] = make_float2(s1, s2);
     }
 }
 
@@ -470,8 +471,9 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormArgs<T> a, unsi
     extern __shared__ __align__(16) float2 stat[];  // [G] m1, m2; or [kThreads]
     const Plan &p = a.p;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    if (blockIdx.x < joins) {
-        const int c = int(blockIdx.x) * kJoined + int(threadIdx.x) % kJoined, row = int(threadIdx.x) / kJoined;
+    const unsigned item = a.first_block + blockIdx.x;
+    if (item < joins) {
+        const int c = int(item) * kJoined + int(threadIdx.x) % kJoined, row = int(threadIdx.x) / kJoined;
         float s1 = 0.f, s2 = 0.f;
         if (c < p.C)
 #pragma unroll 8
@@ -491,7 +493,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormArgs<T> a, unsi
         }
         return;
     }
-    const unsigned block = blockIdx.x - joins, b = block / unsigned(p.strips), strip = block - b * unsigned(p.strips);
+    const unsigned block = item - joins, b = block / unsigned(p.strips), strip = block - b * unsigned(p.strips);
     const int width = p.C / p.G;
     for (int j = w; j < p.G; j += kThreads / 64) {
         const float2 *part = a.partial + size_t(b) * p.strips * p.G + j;
@@ -553,39 +555,53 @@ bool group_in_registers(const Plan &p, int vec)
 }
 
 template <typename T, bool kSilu>
-hipError_t forward(const NormArgs<T> &a, hipStream_t stream)
+hipError_t forward(NormArgs<T> a, hipStream_t stream)
 {
     const Plan &p = a.p;
     const LaunchTimer timer(kKernelGroupNorm, stream);
     if (group_in_registers(p, kVec<T>)) {
         const int pieces = p.L * (p.C / p.G / kVec<T>), each = (pieces + kThreads - 1) / kThreads;
-        const unsigned grid = unsigned(p.B) * unsigned(p.G);
-        if (each <= 1)
-            norm_group_kernel<T, 1, kSilu><<<grid, kThreads, 0, stream>>>(a);
-        else if (each <= 2)
-            norm_group_kernel<T, 2, kSilu><<<grid, kThreads, 0, stream>>>(a);
-        else if (each <= 4)
-            norm_group_kernel<T, 4, kSilu><<<grid, kThreads, 0, stream>>>(a);
-        else
-            norm_group_kernel<T, 8, kSilu><<<grid, kThreads, 0, stream>>>(a);
-        return hipGetLastError();
+        return in_launches(size_t(p.B) * p.G, kThreads, [&](unsigned first, unsigned grid) {
+            a.first_block = first;
+            if (each <= 1)
+                norm_group_kernel<T, 1, kSilu><<<grid, kThreads, 0, stream>>>(a);
+            else if (each <= 2)
+                norm_group_kernel<T, 2, kSilu><<<grid, kThreads, 0, stream>>>(a);
+            else if (each <= 4)
+                norm_group_kernel<T, 4, kSilu><<<grid, kThreads, 0, stream>>>(a);
+            else
+                norm_group_kernel<T, 8, kSilu><<<grid, kThreads, 0, stream>>>(a);
+        });
     }
-    const unsigned grid = unsigned(p.B) * unsigned(p.strips);
-    norm_strip_kernel<T><<<grid, kThreads, size_t(p.row_groups) * p.C * sizeof(float2), stream>>>(a);
-    norm_apply_kernel<T, kSilu><<<grid, kThreads, size_t(p.G) * sizeof(float2), stream>>>(a);
-    return hipGetLastError();
+    const size_t blocks = size_t(p.B) * p.strips;
+    const hipError_t e = in_launches(blocks, kThreads, [&](unsigned first, unsigned grid) {
+        a.first_block = first;
+        norm_strip_kernel<T><<<grid, kThreads, size_t(p.row_groups) * p.C * sizeof(float2), stream>>>(a);
+    });
+    if (e != hipSuccess) return e;
+    return in_launches(blocks, kThreads, [&](unsigned first, unsigned grid) {
+        a.first_block = first;
+        norm_apply_kernel<T, kSilu><<<grid, kThreads, size_t(p.G) * sizeof(float2), stream>>>(a);
+    });
 }
 
 template <typename T, bool kSilu>
-hipError_t backward(const NormArgs<T> &a, hipStream_t stream)
+hipError_t backward(NormArgs<T> a, hipStream_t stream)
 {
     const Plan &p = a.p;
     const LaunchTimer timer(kKernelGroupNormBackward, stream);
-    const unsigned grid = unsigned(p.B) * unsigned(p.strips), joins = a.d_weight ? unsigned(p.C + kJoined - 1) / kJoined : 0;
+    const size_t blocks = size_t(p.B) * p.strips;
+    const unsigned joins = a.d_weight ? unsigned(p.C + kJoined - 1) / kJoined : 0;
     const size_t stat = size_t(p.G > 256 ? p.G : 256) * sizeof(float2);
-    norm_sums_kernel<T, kSilu><<<grid, kThreads, size_t(p.row_groups) * p.C * sizeof(float2), stream>>>(a);
-    norm_grad_kernel<T, kSilu><<<grid + joins, kThreads, stat, stream>>>(a, joins);
-    return hipGetLastError();
+    const hipError_t e = in_launches(blocks, kThreads, [&](unsigned first, unsigned grid) {
+        a.first_block = first;
+        norm_sums_kernel<T, kSilu><<<grid, kThreads, size_t(p.row_groups) * p.C * sizeof(float2), stream>>>(a);
+    });
+    if (e != hipSuccess) return e;
+    return in_launches(blocks + joins, kThreads, [&](unsigned first, unsigned grid) {
+        a.first_block = first;
+        norm_grad_kernel<T, kSilu><<<grid, kThreads, stat, stream>>>(a, joins);
+    });
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }

@@ -76,6 +76,19 @@ hipError_t gate_producer_launch(const void *x, const void *w1, const void *w2, c
 // x W1 alone, bf16: lowrank [B][L][16]
 hipError_t gate_lowrank_launch(const void *x, const void *w1, void *lowrank, int B, int L, int D, hipStream_t stream);
 
+// Launches of `blocks` workgroups of `threads`, run(first, grid) each: a launch has fewer than 2^32 work-items (one of more goes wrong without an error).
+template <typename Run>
+hipError_t in_launches(size_t blocks, unsigned threads, Run run)
+{
+    const size_t most = 0xffffffffu / threads;
+    for (size_t first = 0; first < blocks; first += most) {
+        run(unsigned(first), unsigned(blocks - first < most ? blocks - first : most));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 // ---- gated delta rule ----------------------------------------------------------------------------
 size_t gated_delta_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, bool is_bf16);
 hipError_t gated_delta_launch(const void *q, const void *k, const void *v, const void *g, const void *beta, const float *initial, void *out,
