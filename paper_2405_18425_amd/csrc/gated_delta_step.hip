@@ -15,6 +15,7 @@ namespace {
 template <typename T>
 struct StepArgs {
     int H, Hk, slots_n;
+    unsigned first_block;  // of the launch
     const T *q, *k, *v, *g, *beta;
     float *state;
     const int *slots;
@@ -29,7 +30,7 @@ __global__ __launch_bounds__(256) void gated_delta_step_kernel(StepArgs<T> a)
     constexpr int kRows = kThreads / kQuads, kMine = DK / kRows;         // rows of a pass, of a thread
     constexpr int kWaves = (kThreads + 63) / 64, kLane = kThreads < 64 ? kThreads : 64;
     const int tid = threadIdx.x, quad = tid % kQuads, r0 = tid / kQuads;
-    const unsigned b = blockIdx.x / unsigned(a.H), h = blockIdx.x - b * unsigned(a.H), hk = h / unsigned(a.H / a.Hk);
+    const unsigned block = a.first_block + blockIdx.x, b = block / unsigned(a.H), h = block - b * unsigned(a.H), hk = h / unsigned(a.H / a.Hk);
     const size_t row = size_t(b) * a.H + h;
     T *out = a.out + row * DV;
     static_assert(kThreads >= DV, "");
@@ -86,25 +87,26 @@ __global__ __launch_bounds__(256) void gated_delta_step_kernel(StepArgs<T> a)
 }
 
 template <typename T, int DK>
-hipError_t launch_dv(int dv, int B, const StepArgs<T> &a, hipStream_t stream)
+hipError_t launch_dv(int dv, int B, StepArgs<T> a, hipStream_t stream)
 {
-    const unsigned grid = unsigned(B) * unsigned(a.H);
-    const auto threads = [&](int DV) { return unsigned(DK * DV / 4 < 256 ? DK * DV / 4 : 256); };
     const LaunchTimer timer(kKernelGatedDeltaStep, stream);
-    switch (dv) {
-        case 16: gated_delta_step_kernel<T, DK, 16><<<grid, threads(16), 0, stream>>>(a); break;
-        case 32: gated_delta_step_kernel<T, DK, 32><<<grid, threads(32), 0, stream>>>(a); break;
-        case 64: gated_delta_step_kernel<T, DK, 64><<<grid, threads(64), 0, stream>>>(a); break;
-        default: gated_delta_step_kernel<T, DK, 128><<<grid, threads(128), 0, stream>>>(a); break;
-    }
-    return hipGetLastError();
+    const unsigned threads = unsigned(DK * dv / 4 < 256 ? DK * dv / 4 : 256);
+    return in_launches(size_t(B) * a.H, threads, [&](unsigned first, unsigned grid) {
+        a.first_block = first;
+        switch (dv) {
+            case 16: gated_delta_step_kernel<T, DK, 16><<<grid, threads, 0, stream>>>(a); break;
+            case 32: gated_delta_step_kernel<T, DK, 32><<<grid, threads, 0, stream>>>(a); break;
+            case 64: gated_delta_step_kernel<T, DK, 64><<<grid, threads, 0, stream>>>(a); break;
+            default: gated_delta_step_kernel<T, DK, 128><<<grid, threads, 0, stream>>>(a); break;
+        }
+    });
 }
 
 template <typename T>
 hipError_t launch(const void *q, const void *k, const void *v, const void *g, const void *beta, float *state, const int *slots, void *out, int B, int H,
                   int Hk, int slots_n, int dk, int dv, hipStream_t stream)
 {
-    const StepArgs<T> a = {H, Hk, slots_n, static_cast<const T *>(q), static_cast<const T *>(k), static_cast<const T *>(v), static_cast<const T *>(g),
+    const StepArgs<T> a = {H, Hk, slots_n, 0, static_cast<const T *>(q), static_cast<const T *>(k), static_cast<const T *>(v), static_cast<const T *>(g),
                            static_cast<const T *>(beta), state, slots, static_cast<T *>(out)};
     switch (dk) {
         case 16: return launch_dv<T, 16>(dv, B, a, stream);

@@ -50,3 +50,31 @@ def test_norm_of_more_groups_than_a_launch_has_workgroups(B, C, groups):
     rms = B ** 0.5
     _close(dw, want_dw, rms, "dw")
     _close(db, want_db, rms, "db")
+
+
+def test_steps_of_more_heads_than_a_launch_has_workgroups():
+    """2^20 sequences of 66 heads are 2^26 workgroups of 64 threads; but for some of the first and the last sequences they are padded rows."""
+    from paper_2405_18425_amd import binding as vb
+
+    B, H, Hk, d = 1 << 20, 66, 1, 16
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    n = lambda *s: torch.randn(s, device="cuda", generator=gen, dtype=BF16)
+    q, k, v, g, beta = n(B, Hk, d) * 0.25, n(B, Hk, d) * 0.25, n(B, H, d), -n(B, H).abs(), n(B, H).sigmoid()
+    state = torch.randn(8, H, d, d, device="cuda", generator=gen)
+    before = state.double()
+    slots = torch.full((B,), -1, dtype=torch.int32, device="cuda")
+    live = torch.tensor([0, 5, B // 2, B - 40000, B - 5, B - 1], device="cuda")
+    slots[live] = torch.tensor([3, 0, 7, 1, 6, 2], dtype=torch.int32, device="cuda")
+    out = torch.full_like(v, 77.0)
+    vb.gated_delta_step(q, k, v, g, beta, state, slots=slots, out=out)
+    torch.cuda.synchronize()
+    at = slots[live].long()
+    S = before[at] * g[live].double().exp()[..., None, None]
+    ks = k[live].double().expand(-1, H, -1)
+    u = beta[live].double()[..., None] * (v[live].double() - (ks[..., None] * S).sum(-2))
+    S = S + ks[..., None] * u[..., None, :]
+    _close(out[live], (q[live].double().expand(-1, H, -1)[..., None] * S).sum(-2), 1.0, "out")
+    assert ((state[at].double() - S).abs() <= 2.0 ** -18 * (1 + S.abs())).all()
+    assert torch.equal(state[[4, 5]].double(), before[[4, 5]])  # of no sequence
+    out[live] = 0
+    assert not out.any()  # padded rows
