@@ -327,7 +327,8 @@ int gated_bigla_fwd(const void *x, const void *w1, const void *w2, const void *b
  *   out            [B, H, L, dv]     out
  *   final_state    [B, H, dk, dv]    out   FP32 for either dtype; NULL: not wanted; may be initial_state
  *   (or [B, L, H, d] and [B, L, H] with VIG_LAYOUT_BLHD; states are the same in both); dk, dv in {16, 32, 64, 128}; any L >= 1;
- *   H below 2^15.  Values are finite (gates excepted), as is beta_t |k_t|^2 in [0, 2] where a bounded state is wanted.  A token
+ *   H below 2^15, B H times the 64-token chunks of a sequence below 2^24, B H dv / 16 below 2^25 (the gradient's below 2^24): what a launch
+ *   holds.  Values are finite (gates excepted), as is beta_t |k_t|^2 in [0, 2] where a bounded state is wanted.  A token
  *   with g = 0 and beta = 0 leaves the state as it is: so are padded ones marked.
  *   workspace: at least gated_delta_workspace_bytes(...) bytes (the chunks' matrices), which is 0 for invalid sizes.
  * Chunks of 64 tokens, on the matrix cores for both dtypes.  VIG_BF16: every intermediate operand in two bf16 parts (16 bits), in

@@ -405,11 +405,21 @@ int delta_shape_status(int B, int H, int Hk, int L, int dk, int dv, int dtype)
     if (B <= 0 || H <= 0 || Hk <= 0 || L <= 0 || dk <= 0 || dv <= 0) return VIG_ERR_SHAPE;
     if (dtype != VIG_F32 && dtype != VIG_BF16) return VIG_ERR_DTYPE;
     if (!delta_width_ok(dk) || !delta_width_ok(dv) || H % Hk != 0) return VIG_ERR_UNSUPPORTED;
-    // rows of a chunk are addressed with 32 bits, and a head's 64-token chunks and 16-column parts are workgroups; the
-    // workspace of the gradient is under 128 bytes per token and channel
+    // rows of a chunk are addressed with 32 bits; the workspace of the gradient is under 128 bytes per channel and token of the 64-token chunks (a
+    // sequence of one token has a whole one), and B H below 2^28: no count of its bytes overflows
     if (!sizes_ok(B, H, L, 128L * (dk > dv ? dk : dv)) || H >= (1 << 15) || L >= 0x7fffff00) return VIG_ERR_SHAPE;
-    if ((long(B) * H + 7) * ((long(L) + 63) / 64) > 0x7fffffffL || (long(B) * H + 7) * 8 > 0x7fffffffL) return VIG_ERR_SHAPE;
+    if ((long(B) * H + 7) * 8 > 0x7fffffffL) return VIG_ERR_SHAPE;
     return VIG_OK;
+}
+
+// ... and of a whole sequence's two: their launches have fewer than 2^32 work-items (one of more goes wrong without an error), 256 a chunk of a head, and 128
+// a chain of 16 columns, with `chains` = 1 or the gradient's 2 beside each other.  (Of more chunks a workspace is over 400 GB; of more chains it
+// is over 100 GB, the gradient's over 300.)
+int delta_launch_status(int B, int H, int L, int dv, int chains)
+{
+    const long slabs = long(B) * H;
+    const bool fits = 256 * slabs * ((long(L) + 63) / 64) <= 0xffffffffL && 128 * chains * ((slabs + 7) / 8 * 8 * (dv / 16)) <= 0xffffffffL;
+    return fits ? VIG_OK : VIG_ERR_SHAPE;
 }
 
 bool direction_ok(int direction) { return direction == VIG_SCAN_FORWARD || direction == VIG_SCAN_BACKWARD; }
@@ -418,7 +428,7 @@ bool direction_ok(int direction) { return direction == VIG_SCAN_FORWARD || direc
 
 size_t gated_delta_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, int dtype)
 {
-    if (delta_shape_status(B, H, Hk, L, dk, dv, dtype) != VIG_OK) return 0;
+    if (delta_shape_status(B, H, Hk, L, dk, dv, dtype) != VIG_OK || delta_launch_status(B, H, L, dv, 1) != VIG_OK) return 0;
     return vig::gated_delta_workspace_bytes(B, H, Hk, L, dk, dv, dtype == VIG_BF16);
 }
 
@@ -430,6 +440,7 @@ int gated_delta_fwd(const void *q, const void *k, const void *v, const void *g, 
     if (layout != VIG_LAYOUT_BHLD && layout != VIG_LAYOUT_BLHD) return VIG_ERR_LAYOUT;
     if (!direction_ok(direction)) return VIG_ERR_UNSUPPORTED;
     if (const int st = delta_shape_status(B, H, Hk, L, dk, dv, dtype)) return st;
+    if (const int st = delta_launch_status(B, H, L, dv, 1)) return st;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(g) || !aligned16(beta) || !aligned16(initial_state) || !aligned16(out) ||
         !aligned16(final_state) || !aligned16(workspace))
         return VIG_ERR_ALIGN;
@@ -442,7 +453,7 @@ int gated_delta_fwd(const void *q, const void *k, const void *v, const void *g, 
 
 size_t gated_delta_bwd_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, int dtype)
 {
-    if (delta_shape_status(B, H, Hk, L, dk, dv, dtype) != VIG_OK) return 0;
+    if (delta_shape_status(B, H, Hk, L, dk, dv, dtype) != VIG_OK || delta_launch_status(B, H, L, dv, 2) != VIG_OK) return 0;
     return vig::gated_delta_bwd_workspace_bytes(B, H, Hk, L, dk, dv, dtype == VIG_BF16);
 }
 
@@ -454,6 +465,7 @@ int gated_delta_bwd(const void *q, const void *k, const void *v, const void *g, 
     if (layout != VIG_LAYOUT_BHLD && layout != VIG_LAYOUT_BLHD) return VIG_ERR_LAYOUT;
     if (!direction_ok(direction)) return VIG_ERR_UNSUPPORTED;
     if (const int st = delta_shape_status(B, H, Hk, L, dk_, dv_, dtype)) return st;
+    if (const int st = delta_launch_status(B, H, L, dv_, 2)) return st;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(g) || !aligned16(beta) || !aligned16(initial_state) || !aligned16(d_out) ||
         !aligned16(d_final_state) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(dg) || !aligned16(dbeta) ||
         !aligned16(d_initial_state) || !aligned16(workspace))
