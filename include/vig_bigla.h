@@ -328,11 +328,14 @@ int gated_bigla_fwd(const void *x, const void *w1, const void *w2, const void *b
  *   final_state    [B, H, dk, dv]    out   FP32 for either dtype; NULL: not wanted; may be initial_state
  *   (or [B, L, H, d] and [B, L, H] with VIG_LAYOUT_BLHD; states are the same in both); dk, dv in {16, 32, 64, 128}; any L >= 1;
  *   H below 2^15, B H times the 64-token chunks of a sequence below 2^24, B H dv / 16 below 2^25 (the gradient's below 2^24): what a launch
- *   holds.  Values are finite (gates excepted), as is beta_t |k_t|^2 in [0, 2] where a bounded state is wanted.  A token
- *   with g = 0 and beta = 0 leaves the state as it is: so are padded ones marked.
+ *   holds.  Values are finite, but for gates of -infinity; beta_t |k_t|^2 is in [0, 2] where a bounded state is wanted.  A NaN or
+ *   another infinity may spoil its head from the first token of its 64-token chunk on, in scan order (tokens before it in that chunk
+ *   too), and all its gradients; other heads stay as they are, where they do not share it.  A token with g = 0 and beta = 0
+ *   leaves the state as it is: so are padded ones marked.
  *   workspace: at least gated_delta_workspace_bytes(...) bytes (the chunks' matrices), which is 0 for invalid sizes.
  * Chunks of 64 tokens, on the matrix cores for both dtypes.  VIG_BF16: every intermediate operand in two bf16 parts (16 bits), in
- * three (24 bits) where a final state is asked for; VIG_F32: fp32 operands.
+ * three (24 bits) where a final state is asked for: out then differs by a last bit here and there (one bf16 step, in under
+ * one value of a hundred) from that of a call that does not ask; VIG_F32: fp32 operands.
  */
 typedef enum { VIG_SCAN_FORWARD = 0, VIG_SCAN_BACKWARD = 1 } vig_scan;
 size_t gated_delta_workspace_bytes(int B, int H, int Hk, int L, int dk, int dv, int dtype);
@@ -378,7 +381,10 @@ int gated_delta_step(const void *q, const void *k, const void *v, const void *g,
  *   x, out        [B, L, C]         C a multiple of 8 and of groups, up to VIG_GROUP_NORM_MAX_CHANNELS
  *   weight, bias  [C], or both NULL (one and zero)
  *   stats         [B, groups, 2]    out   FP32 for either dtype: mean and 1 / sqrt(var + eps), what the gradient takes
- *   eps > 0; act a vig_act (VIG_ACT_SILU: z / (1 + exp(-z))); fp32 arithmetic for either dtype.
+ *   eps > 0; act a vig_act (VIG_ACT_SILU: z / (1 + exp(-z))); fp32 arithmetic for either dtype: a variance beyond its range is
+ *   infinite, 1 / sqrt of it 0.  A NaN or infinity in a group makes its statistics and outputs NaN, and no other group's.
+ *   The statistics take in all positions, later ones too: the norm of each token by itself, as tokens are generated, is the call
+ *   with x as [B L, 1, C].
  *   workspace: at least group_norm_workspace_bytes(...) bytes (0 where a group fits one workgroup's registers, and for invalid sizes).
  * group_norm_act_bwd: from d_out = dLoss/dout, dx like x, d_weight and d_bias like weight (NULL exactly where weight is NULL).
  */

@@ -544,7 +544,7 @@ def gated_delta_fwd(q, k, v, g, beta, initial_state=None, return_final_state=Fal
     q, k: [B,Hk,L,dk] with Hk dividing H; v: [B,H,L,dv]; g (log gates), beta: [B,H,L] (layout "bhld"), or [B,L,H,...]
     (layout "blhd"); initial_state: float32 [B,H,dk,dv] or None (zero).  direction "backward" scans from the last token.
     Returns out, or (out, final_state) where the final state is asked for (return_final_state, or a tensor for it, which
-    may be initial_state).
+    may be initial_state); bf16 calls that ask for it work with more bits, and single values of out may differ in the last one.
     """
     sizes, lay, scan = _delta_args(q, k, v, g, beta, layout, direction)
     B, H, Hk, L, dk, dv, code = sizes
@@ -663,7 +663,8 @@ def _norm_args(x, groups, weight, bias, act):
 def group_norm_act_fwd(x, groups: int, weight=None, bias=None, eps: float = 1e-5, act="silu", out=None, stats=None,
                        workspace=None):
     """Channels-last group norm and activation: act((x - mean) / sqrt(var + eps) * weight + bias), the statistics over all
-    positions and the C / groups channels of a group.  x: [B, ..., C]; weight, bias: [C] or both None; act: "silu" or "none".
+    positions (later ones too: for a norm of each token by itself x is [B L, 1, C]) and the C / groups channels of a group.
+    x: [B, ..., C]; weight, bias: [C] or both None; act: "silu" or "none".
     Returns (out, stats), stats: float32 [B, groups, 2], mean and 1 / sqrt(var + eps), for group_norm_act_bwd."""
     sizes, code, act_code = _norm_args(x, groups, weight, bias, act)
     out = torch.empty_like(x) if out is None else _dev(out, "out", x.shape, x)

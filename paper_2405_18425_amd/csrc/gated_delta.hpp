@@ -13,7 +13,8 @@
 // The matrices of a chunk (That, P diag(beta), K^T) do not depend on the state: gd_prepare makes them for all chunks at once.  What is left is a
 // chain of three products a chunk, whose columns (values) are independent: a wave takes 16 of them and keeps its part of the state in registers.
 // (e = That v - (That diag(c) K) S, with both factors prepared, is a chain of two products, 0.87 us a chunk instead of 1.1; but what is prepared is then as
-// wide as the state: 8 x 6 heads of 4096 tokens 106 us against 103, their gradient 363 against 350, 2 x 16 of 8191 with 128 x 128 states 475 against 395.)
+// wide as the state.  Matrices + chain of each form, beside each other, us: 8 x 6 heads of 4096 tokens 50 + 56 against 36 + 74, their gradient 65 + 172
+// against 44 + 187, 2 x 16 of 8191 with 128 x 128 states 106 + 360 against 55 + 347.  The kept form has become faster since; the other was not made again.)
 //
 // v_mfma_f32_16x16x32_bf16, lane (r = l % 16, g = l / 16): A row r and B column r with k = 8g .. 8g + 7; the accumulator holds rows 4g .. 4g + 3 of column
 // r.  Rows of a pair of accumulator tiles stand for the indexes 32p + 8g + 4h + i (tile 2p + h, lane group g, register i), so that the eight
@@ -265,7 +266,7 @@ __device__ __forceinline__ void put(Rsrc ws, size_t first, int block, int lane, 
 }
 // Matrices of more than half the Infinity Cache's 256 MB are written around the caches: little of them would be there when the chains come to it, and what
 // they take would be another's.  (8 x 6 heads of 4096 tokens, gradient, 163 MB: matrices 40 -> 36 us, chains 175 -> 170; 2 x 16 heads of 8191,
-// 128 x 128, 160 MB: chains 308 -> 298.  Below it costs: 8 x 6 of 4096 forward, 101 MB: chains 70 -> 80; 64 x 6 of 196, gradient, 81 MB: 48 -> 66.)
+// 128 x 128, 160 MB: chains 308 -> 298, inputs from the Infinity Cache.  Below it costs: 8 x 6 of 4096 forward, 101 MB: chains 70 -> 80; 64 x 6 of 196, gradient, 81 MB: 48 -> 66.)
 constexpr size_t kStreamedBytes = size_t(128) << 20;
 template <typename Frag>
 __device__ __forceinline__ Frag get(Rsrc ws, size_t first, int block, int lane)

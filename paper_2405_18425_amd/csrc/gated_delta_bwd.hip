@@ -325,8 +325,8 @@ __device__ __forceinline__ void adjoint_sides(const AdjointArgs<T> &a, const Col
     take(0);
 }
 
-// Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'.  8 x 6 heads of 4096 tokens (bf16, 64 x 64): 170 us for 167 MB in and
-// 223 MB out; one chain after the other 87 + 129 us.  A load a line two chunks ahead, to have them in L2, costs more (197 us) than it saves.
+// Two waves per 16 columns of the states' chain (blockIdx.y = 0) and of the adjoints'.  8 x 6 heads of 4096 tokens (bf16, 64 x 64): 167 us for 160 MB in and
+// 222 MB out; one chain after the other 87 + 129 us.  A load a line two chunks ahead, to have them in L2, costs more (197 us) than it saves.
 template <typename T, int DK, int N>
 __global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(chain_waves<T, DK, 1>, chain_waves<T, DK, 1>))) void gd_both_chains(ChainArgs<T> c, AdjointArgs<T> a)
 {
@@ -401,7 +401,7 @@ __device__ __forceinline__ float of_lane(const f32x4 &acc, int r, int g)
 // One chunk of one key head and all value heads that share it, four waves, 16 tokens each.  What more than one wave needs -- rows of k and q, e, the rows
 // of S and D -- each requests a quarter of and all read from LDS; every request of a turn stands before its first wait: one trip to memory
 // a turn.  The contractions over value columns take kSlice of them at a time.  Bound by the phases of two waves a SIMD (64 x 64, bf16: 1200 vector and 180 matrix
-// instructions each, ten phases between barriers): 8 x 6 heads of 4096 tokens take 79 us, and 90 in
+// instructions each, ten phases between barriers): 8 x 6 heads of 4096 tokens take 77 us, and 90 in
 // workgroups that go on to another chunk with its requests under way.
 // kOne: the values are one slice; two workgroups then fit a compute unit's registers (without it the accumulators are live across the
 // requests of the next slice, and what spills costs more than the second workgroup brings).

@@ -6,7 +6,8 @@
 // XCD (blockIdx % 8), whose L2 they read the fragments from.
 //
 // What bounds it (64 x 64, bf16): where every workgroup has a compute unit, its own instructions, 50 matrix and 225 vector ones a chunk in one wave, 1.1 us
-// (8 x 6 heads of 4096 tokens: 70 us; 66 without a request in the loop, 63 without the outputs' either).  With several workgroups on a compute unit, what
+// (8 x 6 heads of 4096 tokens: 70 us with inputs in the Infinity Cache, 66 without a request in the loop, 63 without the outputs' either; 85 us with inputs from
+// memory).  With several workgroups on a compute unit, what
 // comes through its first-level cache, 50 KB a chunk and 16 columns: 16 x 16 heads of 1024 tokens take 79 us, 35 without requests.  Two groups of columns
 // in a wave take twice as long a step; two in a workgroup read the same lines at different times (115 us instead of 74).
 #pragma once
@@ -164,7 +165,7 @@ __device__ __forceinline__ void strip_column(float (&x)[8], const unsigned char 
 // What the chains of the gradient leave: a state (DK rows) or 64 tokens' rows, 16 columns a wave, first in LDS as [column][row] tiles of floats, which a
 // second wave takes to the workspace as fragments of two parts: rows by 16 in tiles, columns along the products.  By non-temporal stores: read by the
 // next launch only, they leave the L2 to the fragments that the columns of a head share (chains of 8 x 6 heads of 4096 tokens 185 -> 173 us, 64 x 6 of 196
-// 54.5 -> 48).
+// 54.5 -> 48, inputs in the Infinity Cache).
 template <int kRows>
 struct Tile {
     static constexpr int pitch = kRows + 4, bytes = 16 * pitch * 4;

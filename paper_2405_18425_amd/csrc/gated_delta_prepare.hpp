@@ -1,12 +1,13 @@
 // gd_prepare: the matrices of a chunk that do not depend on the state, one workgroup of four waves per chunk of one head.
 //
-// K K^T and Q K^T on the matrix cores, a 16-row strip a wave, lower triangle only; That = (1 + N diag(beta))^-1 in 32-bit arithmetic:
+// K K^T and Q K^T on the matrix cores, a 16-row strip a wave (all four tiles of it: the last wave needs them, and the others lose less
+// than by branches); That = (1 + N diag(beta))^-1 in 32-bit arithmetic:
 // the four 16 x 16 diagonal blocks by substitution, a wave each (lane: a column), then two joins [[A, 0], [-B C A, B]] of
 // blocks twice as large, on v_mfma_f32_16x16x4_f32.  A substitution divides by nothing and a join only multiplies
 // inverses, so keys that repeat (N full of ones) lose no more than the recurrence itself does.
 //
-// Bound by memory where there are many chunks: of 8 x 6 heads of 4096 tokens (bf16, 64 x 64) it reads 50 MB and writes 101 in 32.5 us, 4.7 TB/s; for the
-// gradient 163 MB in 36 us.  Of one sequence of 196 tokens it is the latency of its steps, 7 us.
+// Bound by memory where there are many chunks: of 8 x 6 heads of 4096 tokens (bf16, 64 x 64) it reads 50 MB and writes 101 in 35.4 us, 4.3 TB/s; for the
+// gradient it writes 163 MB in 43 us.  Of one sequence of 196 tokens it is the latency of its steps, 7.5 us.
 #pragma once
 
 #include "gated_delta.hpp"

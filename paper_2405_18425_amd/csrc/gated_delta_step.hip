@@ -3,7 +3,8 @@
 // Bound by the state: dk x dv floats read and written once.  A thread owns four neighbouring columns of every kRows-th row, so a wave reads whole
 // rows, and keeps them in registers from the read to the write.  Both products with the old state, k S and q S, are summed in one
 // pass and joined once through LDS: with the written correction u, o = a q S + (q . k) u.
-// 117 sequences of 16 heads with 128 x 128 states: 246 MB in 48.9 us, 5.05 TB/s (a large copy reaches 4.8).  One sequence: what a launch costs.
+// 117 sequences of 16 heads with 128 x 128 states: 246 MB in 55 us from memory, 4.5 TB/s (a large copy reaches 4.8), 38 us where the Infinity Cache holds
+// part of the pool from the call before.  One sequence: what a launch costs.
 #include "vig_common.hpp"
 #include "vig_kernels.hpp"
 #include "vig_timing.hpp"

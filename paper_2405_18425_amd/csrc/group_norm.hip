@@ -9,8 +9,11 @@
 // element themselves (the same order in each, so results do not depend on the launch); the second reading of x comes from
 // the Infinity Cache up to its size.  A thread owns 16 bytes of channels of every RG-th row, so a wave reads whole rows whatever the group width.
 //
-// Measured (bf16): 8 x 4096 x 384 in 6 groups 9.8 + 11.6 us, 25 MB in, 25 MB in again and 25 MB out: 2.6 and 4.3 TB/s; 16 x 3136 x 128 in 2 groups, gradient,
-// 10.3 + 9.5 us; 64 x 49 x 1024 in 16 groups, one launch, 7.0 us for 13 MB, mostly the latency of one trip in, the sums and one trip out.
+// Measured (bf16, inputs from memory, medians): 8 x 4096 x 384 in 6 groups 10.4 + 11.2 us, 25 MB in, 25 MB in again and 25 MB out: 2.4 and 4.5 TB/s;
+// 16 x 3136 x 128 in 2 groups, gradient, 10.8 + 9.3 us; 64 x 49 x 1024 in 16 groups, one launch, 7.1 us for 13 MB, mostly the latency of one trip in, the sums and
+// one trip out.  Far from the data's time: the gradient of few elements with many groups, whose workgroups each read all strips' sums at a stride
+// (1 x 4096 x 2048 in 32 groups: 83 us for 50 MB; the forward, whose pairs lie by group, 37), and groups of few values, a workgroup of 256 threads each
+// (16384 x 1 x 1024 in 16 groups: 269 us, gradient 165).
 //
 // Variances are sums of terms that are not negative, never a difference: runs of four rows, a strip's channels and threads and the strips are
 // joined by the squared distances of their means from the mean of all, which a pass before has.  (From the first of those means, as one pass would have

@@ -414,7 +414,7 @@ int delta_shape_status(int B, int H, int Hk, int L, int dk, int dv, int dtype)
 
 // ... and of a whole sequence's two: their launches have fewer than 2^32 work-items (one of more goes wrong without an error), 256 a chunk of a head, and 128
 // a chain of 16 columns, with `chains` = 1 or the gradient's 2 beside each other.  (Of more chunks a workspace is over 400 GB; of more chains it
-// is over 100 GB, the gradient's over 300.)
+// is over 100 GB, the gradient's over 280.)
 int delta_launch_status(int B, int H, int L, int dv, int chains)
 {
     const long slabs = long(B) * H;
