@@ -13,7 +13,7 @@ NAMES = ("q", "k", "v", "g", "beta")
 
 @pytest.mark.parametrize("direction", ("forward", "backward"))
 def test_gradient_with_matrices_around_the_caches(direction):
-    """3072 chunks of heads of 64 x 64: 163 MB of matrices, over the 128 MB from which they are streamed."""
+    """48 heads of 64 chunks of 64 x 64: 163 MB of matrices, over the 128 MB from which they are streamed."""
     from paper_2405_18425_amd import binding as vb
 
     t = _delta(8, 6, 6, 4096, 64, 64, BF16, states=False, seed=1)
